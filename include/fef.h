@@ -58,7 +58,7 @@ extern "C" {
 
 #define FEF_MAX_K 64
 #define FEF_MAX_BLOCK 4096
-#define FEF_ABI_VERSION 10
+#define FEF_ABI_VERSION 11
 #define FEF_STATIC_SCRATCH_BYTES (32u << 20) /* built-in scratch of fef_verify_step_static        */
 
 typedef enum {
@@ -259,6 +259,68 @@ int32_t fef_select_gemm(const fef_params* prm, int32_t K);
 size_t fef_cross_entropy_workspace_bytes(const fef_params* prm, int32_t R);
 fef_status fef_head_cross_entropy(const fef_params* prm, const void* h, const void* W_vocab,
                                   const int32_t* labels, int32_t R, float* out_ce, float* out_loss);
+
+/* Logits of the vocabulary head from a copy of W in 4 bits (the OCP MX form, MXFP4):
+ *   out_logits[r, v] = (1 / tau) sum_k h[r, k] w[v, k],   w[v, k] = e2m1(code[v, k]) 2^(scale[v, k / 32] - 127)
+ * The draft half of a round may read such a copy instead of W (17/64 of the bytes): a round stays exact whatever law its
+ * drafts come from, as long as the accept test knows that law (fef_verify_logits).
+ *   h          [R, d]      device, dtype prm->dtype (bf16 or f32), 16-byte aligned
+ *   codes      [V, d / 2]  device bytes, 16-byte aligned: two e2m1 codes each, the low nibble is the even k; a code is a sign bit
+ *                          over the magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6
+ *   scales     [V, d / 32] device bytes, 16-byte aligned: e8m0, one power of two per 32 codes; 255 is NaN and makes its token's logits NaN
+ *   out_logits [R, ld]     device float, 4-byte aligned, ld >= V; columns from V on are not touched
+ * w and bf16 hidden states are exact in the multiply, float32 ones too (taken as three bf16 parts; what lies below 2^-133 is lost);
+ * sums are held in 32 bits, in an order that the sizes decide.
+ * Fields of prm that are read: struct_size, d (a positive multiple of 32), V, dtype, temperature, stream, ev_head_begin /
+ * ev_head_end (around the kernel).  1 <= R <= 2^24.  No workspace.  Same conventions and error behaviour as fef_verify_step. */
+fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* codes, const uint8_t* scales, int32_t R,
+                          float* out_logits, int64_t ld);
+
+/* Edits of logits between a head and the token law: penalties for tokens that occurred, biases, grammar masks.  For slot m of
+ * sequence b let n(v) be how often token v occurs in history[b, prompt_len[b] : history_len[b]] and prefix[b, 0 : m] together, and
+ * seen(v) be true if n(v) > 0 or v occurs in the prompt history[b, 0 : prompt_len[b]].  A logit x of token v becomes
+ *   x / repetition[b] if x > 0, else x * repetition[b]         where seen(v)
+ *   minus frequency[b] n(v), minus presence[b] where n(v) > 0
+ *   plus the biases of v (all entries of b's list that name it, in their order)
+ *   times 1 / tau
+ *   -inf where the slot's bit mask does not allow v
+ * computed in float32.  Ids outside [0, V) in any list (-1 pads a list) stand for no token. */
+typedef struct {
+  uint32_t struct_size;        /* = sizeof(fef_edit_params)                                        */
+  int32_t B, K, V;             /* sequences, window slots (<= FEF_MAX_K), vocabulary               */
+  int32_t dtype;               /* fef_dtype of the logits                                          */
+  float temperature;           /* tau > 0                                                          */
+  int64_t seq_stride;          /* elements from a sequence's logits to the next one's, >= 0        */
+  int64_t slot_stride;         /* elements from a slot's logits to the next one's, >= 0            */
+  int64_t out_seq_stride;      /* the same of the output; rows of the output must not overlap      */
+  int64_t out_slot_stride;
+  int32_t history_max;         /* columns of history; 0: no history                                */
+  const int32_t* history;      /* [B, history_max], NULL with history_max == 0                     */
+  const int32_t* history_len;  /* [B] tokens in use, clamped to [0, history_max]; NULL: all        */
+  const int32_t* prompt_len;   /* [B] of these the prompt, clamped to history_len; NULL: none      */
+  const int32_t* prefix;       /* [B, K] token assumed at each slot (slot m sees those before m); NULL: none */
+  const float* repetition;     /* [B] each, NULL: 1, 0 and 0                                       */
+  const float* presence;
+  const float* frequency;
+  int32_t n_bias;              /* entries of a bias list; 0: no biases                             */
+  const int32_t* bias_ids;     /* [B, n_bias]                                                      */
+  const float* bias_values;    /* [B, n_bias]                                                      */
+  int32_t masks;               /* 0: no masks, 1: one per sequence, K: one per slot                */
+  const uint32_t* allowed;     /* [B, masks, ceil(V / 32)]: bit v % 32 of word v / 32 allows token v */
+  void* workspace;             /* device scratch, 256-byte aligned                                 */
+  size_t workspace_bytes;
+  void* stream;                /* hipStream_t; NULL = the null stream                              */
+} fef_edit_params;
+
+/* Bytes of device workspace fef_edit_logits needs (depends on B, K, V alone); 0 if the arguments are invalid. */
+size_t fef_edit_workspace_bytes(const fef_edit_params* prm);
+
+/*   logits  [B, K, V] device, strides above, aligned to its elements
+ *   out     [B, K, V] device float, strides above: the edited logits.  May be `logits` itself where those are float32
+ *                     and the strides are the same; must not overlap it otherwise
+ *   out_lse [B, K]    device float, contiguous: log-sum-exp of each row, -inf for one that leaves no token; may be NULL
+ * Conventions and error behaviour as in fef_verify_step. */
+fef_status fef_edit_logits(const fef_edit_params* prm, const void* logits, float* out, float* out_lse);
 
 /* Philox4x32-10 word 0 -> uniform, evaluated on the host with the same code the kernels
  * use; lets callers and tests reproduce a draw.  Pure host function. */

@@ -21,12 +21,12 @@ FEF_GEMM_ROWSTREAM = 6
 FEF_MAX_K, FEF_MAX_BLOCK = 64, 4096
 FEF_PHASE_FUSED, FEF_PHASE_DRAFT, FEF_PHASE_TARGET = 0, 1, 2
 
-ABI_VERSION = 10   # FEF_ABI_VERSION of include/fef.h this binding's fef_params mirrors
+ABI_VERSION = 11   # FEF_ABI_VERSION of include/fef.h this binding's fef_params mirrors
 
 EXPORTS = ["fef_workspace_bytes", "fef_verify_step", "fef_select_gemm", "fef_uniform",
            "fef_status_string", "fef_last_error", "fef_abi_version", "fef_copy_probe", "fef_read_probe",
            "fef_cross_entropy_workspace_bytes", "fef_head_cross_entropy", "fef_topn_step",
-           "fef_verify_step_static"]
+           "fef_verify_step_static", "fef_mx4_logits", "fef_edit_workspace_bytes", "fef_edit_logits"]
 FEF_STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -56,6 +56,27 @@ class fef_params(ctypes.Structure):
 _PARAMS_SIZE = ctypes.sizeof(fef_params)
 _DIAG = ("draft_tokens", "alpha", "resid_mass", "lse", "logits", "conf_tok")  # VerifyStep.diag in the order of the fields
 _NO_DIAG = (None,) * len(_DIAG)
+
+
+class fef_edit_params(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("B", ctypes.c_int32), ("K", ctypes.c_int32), ("V", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("temperature", ctypes.c_float),
+        ("seq_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64),
+        ("out_seq_stride", ctypes.c_int64), ("out_slot_stride", ctypes.c_int64),
+        ("history_max", ctypes.c_int32), ("history", ctypes.c_void_p),
+        ("history_len", ctypes.c_void_p), ("prompt_len", ctypes.c_void_p), ("prefix", ctypes.c_void_p),
+        ("repetition", ctypes.c_void_p), ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p),
+        ("n_bias", ctypes.c_int32), ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p),
+        ("masks", ctypes.c_int32), ("allowed", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+_EDIT_PARAMS_SIZE = ctypes.sizeof(fef_edit_params)
 
 
 class FefError(RuntimeError):
@@ -108,6 +129,13 @@ def lib():
         L.fef_head_cross_entropy.restype = ctypes.c_int
         L.fef_head_cross_entropy.argtypes = [ctypes.POINTER(fef_params), ctypes.c_void_p, ctypes.c_void_p,
                                              ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]
+        L.fef_mx4_logits.restype = ctypes.c_int
+        L.fef_mx4_logits.argtypes = [ctypes.POINTER(fef_params), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                     ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64]
+        L.fef_edit_workspace_bytes.restype = ctypes.c_size_t
+        L.fef_edit_workspace_bytes.argtypes = [ctypes.POINTER(fef_edit_params)]
+        L.fef_edit_logits.restype = ctypes.c_int
+        L.fef_edit_logits.argtypes = [ctypes.POINTER(fef_edit_params), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
         if L.fef_abi_version() != ABI_VERSION:
             raise RuntimeError(f"{LIB_PATH} has ABI version {L.fef_abi_version()}, this binding needs {ABI_VERSION}: "
                                "rebuild it with `python -m paper_2605_14305_amd.build`")
@@ -356,3 +384,101 @@ class BlockDecoder:
                 seq_pass=self.seq_pass, seq_rounds=self.seq_rounds, tokens_state=self.tokens, **kw)
         # out_remask of this round is the mask of the next one (device-to-device, stream ordered)
         self.mask.copy_(self.vs.out_remask)
+
+
+class Mx4Logits:
+    """Logits of R rows through a vocabulary head held in 4 bits (fef_mx4_logits): codes [V, d / 2] and scales [V, d / 32], both
+    uint8.  Holds the output of one shape; a call returns it (float32 [R, V]), or `out` if the caller gives one, whose rows may lie
+    further apart."""
+
+    def __init__(self, R, d, V, dtype="bf16", device="cuda"):
+        self.R, self.d, self.V, self.device = R, d, V, torch.device(device)
+        self.dtype = FEF_BF16 if dtype == "bf16" else FEF_F32
+        self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.out = torch.empty(R, V, dtype=torch.float32, device=self.device)
+        self._params = make_params(1, d, V, dtype=self.dtype)
+
+    def __call__(self, h, codes, scales, temperature=1.0, out=None, head_events=None):
+        R, d, V = self.R, self.d, self.V
+        if out is None:
+            out = self.out
+        assert h.shape == (R, d) and h.dtype == self.torch_dtype
+        assert codes.shape == (V, d // 2) and scales.shape == (V, d // 32) and codes.dtype == scales.dtype == torch.uint8
+        assert out.shape == (R, V) and out.dtype == torch.float32 and (V == 1 or out.stride(1) == 1)
+        for t in (h, codes, scales):
+            assert t.is_contiguous() and t.is_cuda
+        assert out.is_cuda
+        p = self._params
+        p.temperature = temperature
+        p.stream = _stream(self.device)
+        p.ev_head_begin, p.ev_head_end = head_events if head_events is not None else (None, None)
+        s = (_lib or lib()).fef_mx4_logits(p, h.data_ptr(), codes.data_ptr(), scales.data_ptr(), R, out.data_ptr(),
+                                           out.stride(0) if R > 1 else V)
+        if s != FEF_OK:
+            raise FefError(s, fef_last_error())
+        return out
+
+
+class Edits:
+    """What is done to the logits of B sequences (fef_edit_logits says what each means); everything is optional.
+    history [B, H], history_len [B], prompt_len [B], prefix [B, K], bias_ids [B, n]: int32; repetition, presence, frequency [B],
+    bias_values [B, n]: float32; allowed [B, 1 or K, ceil(V / 32)]: int32, bit v % 32 of word v / 32.  Holds the tensors; their
+    contents may change between calls."""
+
+    _DTYPES = {"history": torch.int32, "history_len": torch.int32, "prompt_len": torch.int32, "prefix": torch.int32,
+               "repetition": torch.float32, "presence": torch.float32, "frequency": torch.float32,
+               "bias_ids": torch.int32, "bias_values": torch.float32, "allowed": torch.int32}
+    __slots__ = tuple(_DTYPES)
+
+    def __init__(self, history=None, history_len=None, prompt_len=None, prefix=None, repetition=None, presence=None,
+                 frequency=None, bias_ids=None, bias_values=None, allowed=None):
+        given = (history, history_len, prompt_len, prefix, repetition, presence, frequency, bias_ids, bias_values, allowed)
+        for (name, dtype), t in zip(self._DTYPES.items(), given):
+            assert t is None or t.dtype == dtype, f"{name} must be {dtype}"
+            setattr(self, name, t)
+        assert (bias_ids is None) == (bias_values is None), "bias_ids and bias_values belong together"
+        assert history is not None or (history_len is None and prompt_len is None), "lengths of no history"
+
+
+class EditLogits:
+    """Edits of logits [B, K, V] of `dtype` ("f32" or "bf16", any strides whose last is 1).  Holds workspace, output (float32
+    [B, K, V]) and log-sum-exps [B, K] of one shape; a call returns both outputs.  `out` may be given, and may be the logits."""
+
+    def __init__(self, B, K, V, dtype="f32", device="cuda"):
+        self.B, self.K, self.V, self.device = B, K, V, torch.device(device)
+        self.dtype = FEF_BF16 if dtype == "bf16" else FEF_F32
+        self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        p = fef_edit_params(struct_size=_EDIT_PARAMS_SIZE, B=B, K=K, V=V, dtype=self.dtype, temperature=1.0,
+                            seq_stride=K * V, slot_stride=V, out_seq_stride=K * V, out_slot_stride=V)
+        n = lib().fef_edit_workspace_bytes(ctypes.byref(p))
+        if n == 0:
+            raise FefError(FEF_ERR_INVALID_ARG, fef_last_error())
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self.out = torch.empty(B, K, V, dtype=torch.float32, device=self.device)
+        self.out_lse = torch.empty(B, K, dtype=torch.float32, device=self.device)
+
+    def __call__(self, logits, edits, temperature=1.0, out=None):
+        B, K, V = self.B, self.K, self.V
+        if out is None:
+            out = self.out
+        for t, dt in ((logits, self.torch_dtype), (out, torch.float32)):
+            assert t.shape == (B, K, V) and t.dtype == dt and t.is_cuda and (V == 1 or t.stride(2) == 1)
+        e = edits
+        H = e.history.shape[1] if e.history is not None else 0
+        n_bias = e.bias_ids.shape[1] if e.bias_ids is not None else 0
+        masks = e.allowed.shape[1] if e.allowed is not None else 0
+        for t, shape in ((e.history, (B, H)), (e.history_len, (B,)), (e.prompt_len, (B,)), (e.prefix, (B, K)),
+                         (e.repetition, (B,)), (e.presence, (B,)), (e.frequency, (B,)), (e.bias_ids, (B, n_bias)),
+                         (e.bias_values, (B, n_bias)), (e.allowed, (B, masks, (V + 31) // 32))):
+            if t is not None:
+                assert t.shape == shape and t.is_contiguous() and t.is_cuda
+        assert masks in (0, 1, K)
+        p = fef_edit_params(_EDIT_PARAMS_SIZE, B, K, V, self.dtype, temperature, logits.stride(0), logits.stride(1),
+                            out.stride(0), out.stride(1), H, _ptr(e.history), _ptr(e.history_len), _ptr(e.prompt_len),
+                            _ptr(e.prefix), _ptr(e.repetition), _ptr(e.presence), _ptr(e.frequency), n_bias,
+                            _ptr(e.bias_ids), _ptr(e.bias_values), masks, _ptr(e.allowed), self.workspace.data_ptr(),
+                            self.workspace.numel(), _stream(self.device))
+        s = (_lib or lib()).fef_edit_logits(p, logits.data_ptr(), out.data_ptr(), self.out_lse.data_ptr())
+        if s != FEF_OK:
+            raise FefError(s, fef_last_error())
+        return out, self.out_lse

@@ -515,6 +515,106 @@ fef_status fef_head_cross_entropy(const fef_params* prm, const void* h, const vo
   return FEF_OK;
 }
 
+fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* codes, const uint8_t* scales, int32_t R,
+                          float* out_logits, int64_t ld) {
+  if (!prm) return fail(FEF_ERR_INVALID_ARG, "params is NULL");
+  if (prm->struct_size != sizeof(fef_params))
+    return fail(FEF_ERR_INVALID_ARG, "struct_size %u does not match this library's %zu", prm->struct_size, sizeof(fef_params));
+  if (R < 1 || R > (1 << 24)) return fail(FEF_ERR_INVALID_ARG, "R = %d out of range [1, 2^24]", R);
+  if (prm->V < 1 || prm->d < 1) return fail(FEF_ERR_INVALID_ARG, "V and d must be positive");
+  if (prm->d % 32 != 0) return fail(FEF_ERR_INVALID_ARG, "a 4-bit head needs d to be a multiple of 32 (got %d)", prm->d);
+  if (prm->dtype != FEF_BF16 && prm->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", prm->dtype);
+  if (!(prm->temperature > 0.f) || !(prm->temperature < 1e30f))
+    return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number");
+  if (!h || !codes || !scales || !out_logits) return fail(FEF_ERR_INVALID_ARG, "h, codes, scales and out_logits must not be NULL");
+  if (((uintptr_t)h | (uintptr_t)codes | (uintptr_t)scales) & 15)
+    return fail(FEF_ERR_INVALID_ARG, "h, codes and scales must be 16-byte aligned");
+  if ((uintptr_t)out_logits & 3) return fail(FEF_ERR_INVALID_ARG, "out_logits must be 4-byte aligned");
+  if (ld < prm->V || ld > (1L << 40)) return fail(FEF_ERR_INVALID_ARG, "ld = %ld must lie in [V, 2^40]", (long)ld);
+  if (!prm->ev_head_begin != !prm->ev_head_end)
+    return fail(FEF_ERR_INVALID_ARG, "ev_head_begin and ev_head_end must be given together");
+  fef::Mx4Args a{};
+  a.h = h; a.codes = codes; a.scales = scales;
+  a.R = R; a.d = prm->d; a.V = prm->V; a.f32 = prm->dtype == FEF_F32;
+  a.inv_tau = 1.0f / prm->temperature;
+  a.logits = out_logits; a.ld = ld;
+  a.stream = (hipStream_t)prm->stream;
+  a.ev_begin = (hipEvent_t)prm->ev_head_begin; a.ev_end = (hipEvent_t)prm->ev_head_end;
+  const hipError_t e = fef::launch_mx4(a);
+  if (e != hipSuccess) return fail(FEF_ERR_HIP, "4-bit head kernel launch: %s", hipGetErrorString(e));
+  return FEF_OK;
+}
+
+namespace {
+fef_status check_edit(const fef_edit_params* p, size_t* total) {
+  if (!p) return fail(FEF_ERR_INVALID_ARG, "params is NULL");
+  if (p->struct_size != sizeof(fef_edit_params))
+    return fail(FEF_ERR_INVALID_ARG, "struct_size %u does not match this library's %zu", p->struct_size, sizeof(fef_edit_params));
+  if (p->B < 1 || p->V < 1) return fail(FEF_ERR_INVALID_ARG, "B and V must be >= 1 (got %d, %d)", p->B, p->V);
+  if (p->K < 1 || p->K > FEF_MAX_K) return fail(FEF_ERR_INVALID_ARG, "K = %d out of range [1, %d]", p->K, FEF_MAX_K);
+  if ((long)p->B * p->K > (1L << 24)) return fail(FEF_ERR_INVALID_ARG, "B*K = %ld exceeds 2^24 rows per call", (long)p->B * p->K);
+  if (p->dtype != FEF_BF16 && p->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
+  if (!(p->temperature > 0.f) || !(p->temperature < 1e30f))
+    return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number");
+  if (p->history_max < 0 || p->n_bias < 0) return fail(FEF_ERR_INVALID_ARG, "history_max and n_bias must not be negative");
+  if (p->masks != 0 && p->masks != 1 && p->masks != p->K)
+    return fail(FEF_ERR_INVALID_ARG, "masks must be 0, 1 or K (got %d)", p->masks);
+  for (const int64_t s : {p->seq_stride, p->slot_stride, p->out_seq_stride, p->out_slot_stride})
+    if (s < 0 || s > (1L << 40)) return fail(FEF_ERR_INVALID_ARG, "strides must lie in [0, 2^40]");
+  // rows of the output one behind another, slots inside sequences or sequences inside slots
+  const int64_t sq = p->out_seq_stride, sl = p->out_slot_stride;
+  const bool apart = (p->K == 1 || sl >= p->V) && (p->B == 1 || sq >= p->V) &&
+                     (p->K == 1 || p->B == 1 || sq >= sl * (p->K - 1) + p->V || sl >= sq * (p->B - 1) + p->V);
+  if (!apart) return fail(FEF_ERR_INVALID_ARG, "rows of the output overlap");
+  *total = align_up((size_t)p->B * p->K * (size_t)fef::edit_partials(p->V) * sizeof(float2), 256);
+  return FEF_OK;
+}
+}  // namespace
+
+size_t fef_edit_workspace_bytes(const fef_edit_params* prm) {
+  size_t total;
+  return check_edit(prm, &total) == FEF_OK ? total : 0;
+}
+
+fef_status fef_edit_logits(const fef_edit_params* p, const void* logits, float* out, float* out_lse) {
+  size_t total;
+  const fef_status s = check_edit(p, &total);
+  if (s != FEF_OK) return s;
+  if (!logits || !out) return fail(FEF_ERR_INVALID_ARG, "logits and out must not be NULL");
+  if ((uintptr_t)logits & (p->dtype == FEF_BF16 ? 1 : 3) || (uintptr_t)out & 3 || (uintptr_t)out_lse & 3)
+    return fail(FEF_ERR_INVALID_ARG, "logits, out and out_lse must be aligned to their elements");
+  if ((const void*)out == logits &&
+      (p->dtype != FEF_F32 || (p->B > 1 && p->seq_stride != p->out_seq_stride) || (p->K > 1 && p->slot_stride != p->out_slot_stride)))
+    return fail(FEF_ERR_INVALID_ARG, "editing in place needs float32 logits and the same strides");
+  if (p->history_max > 0 && !p->history) return fail(FEF_ERR_INVALID_ARG, "history is NULL with history_max %d", p->history_max);
+  if (p->n_bias > 0 && (!p->bias_ids || !p->bias_values)) return fail(FEF_ERR_INVALID_ARG, "bias_ids and bias_values must not be NULL with n_bias %d", p->n_bias);
+  if (p->masks > 0 && !p->allowed) return fail(FEF_ERR_INVALID_ARG, "allowed is NULL with masks %d", p->masks);
+  const uintptr_t lists = (uintptr_t)p->history | (uintptr_t)p->history_len | (uintptr_t)p->prompt_len | (uintptr_t)p->prefix |
+                          (uintptr_t)p->repetition | (uintptr_t)p->presence | (uintptr_t)p->frequency | (uintptr_t)p->bias_ids |
+                          (uintptr_t)p->bias_values | (uintptr_t)p->allowed;
+  if (lists & 3) return fail(FEF_ERR_INVALID_ARG, "lists, penalties and masks must be 4-byte aligned");
+  if (!p->workspace) return fail(FEF_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", total);
+  if ((uintptr_t)p->workspace & 255) return fail(FEF_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (p->workspace_bytes < total) return fail(FEF_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", p->workspace_bytes, total);
+  fef::EditArgs a{};
+  a.B = p->B; a.K = p->K; a.V = p->V; a.bf16 = p->dtype == FEF_BF16;
+  a.inv_tau = 1.0f / p->temperature;
+  a.logits = logits; a.seq_stride = p->seq_stride; a.slot_stride = p->slot_stride;
+  a.out = out; a.out_seq_stride = p->out_seq_stride; a.out_slot_stride = p->out_slot_stride;
+  if (p->repetition || p->presence || p->frequency) {  // without penalties nothing depends on what occurred
+    a.history_max = p->history_max; a.history = p->history; a.history_len = p->history_len; a.prompt_len = p->prompt_len;
+    a.prefix = p->prefix;
+    a.repetition = p->repetition; a.presence = p->presence; a.frequency = p->frequency;
+  }
+  a.n_bias = p->n_bias; a.bias_ids = p->bias_ids; a.bias_values = p->bias_values;
+  a.masks = p->masks; a.allowed = p->allowed;
+  a.partials = (float2*)p->workspace; a.out_lse = out_lse;
+  a.stream = (hipStream_t)p->stream;
+  const hipError_t e = fef::launch_edit(a);
+  if (e != hipSuccess) return fail(FEF_ERR_HIP, "edit kernel launch: %s", hipGetErrorString(e));
+  return FEF_OK;
+}
+
 float fef_uniform(uint64_t seed, uint32_t position, uint32_t step, uint32_t sequence, uint32_t stream) {
   return fef::philox_uniform(seed, position, step, sequence, stream);
 }

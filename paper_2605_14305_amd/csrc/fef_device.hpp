@@ -159,4 +159,40 @@ struct CeArgs {
 };
 hipError_t launch_ce_finish(const CeArgs& a);
 
+// Logits from a head in 4 bits (MXFP4): codes [V, d / 2], scales [V, d / 32].
+struct Mx4Args {
+  const void* h;  // [R, d] bf16 or f32
+  const uint8_t *codes, *scales;
+  int R, d, V, f32;
+  float inv_tau;
+  float* logits;  // [R, ld]
+  long ld;
+  hipStream_t stream;
+  hipEvent_t ev_begin, ev_end;
+};
+hipError_t launch_mx4(const Mx4Args& a);
+
+// Edits of logits (fef_edit_params of the C ABI), one row per (sequence, slot).
+struct EditArgs {
+  int B, K, V, bf16;
+  float inv_tau;
+  const void* logits;
+  long seq_stride, slot_stride;
+  float* out;
+  long out_seq_stride, out_slot_stride;
+  int history_max;
+  const int32_t *history, *history_len, *prompt_len, *prefix;
+  const float *repetition, *presence, *frequency;
+  int n_bias;
+  const int32_t* bias_ids;
+  const float* bias_values;
+  int masks;
+  const uint32_t* allowed;
+  float2* partials;  // [B*K, edit_partials(V)]
+  float* out_lse;    // [B*K] or NULL
+  hipStream_t stream;
+};
+int edit_partials(int V);  // (max, sum exp) pairs per row
+hipError_t launch_edit(const EditArgs& a);
+
 }  // namespace fef
