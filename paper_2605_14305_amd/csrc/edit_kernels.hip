@@ -14,153 +14,248 @@
 // multiplied: a row of nothing but -inf sums to 0 and ends at -inf, one of the type's lowest value keeps it, +inf gives +inf, NaN NaN.
 #include <float.h>
 
-#include "head_common.hpp"
+#include "fef_device.hpp"
 #include "wave_ops.hpp"
+
 
 namespace fef {
 namespace {
 
-constexpr int NT = 256, NW = NT / kWave;
-constexpr int kPer = 8;              // tokens per thread: two runs of four
-constexpr int kChunk = NT * kPer;
+constexpr int kPer = 8;                   // tokens per thread: two runs of four
 constexpr unsigned kInPrompt = 1u << 31;  // of a table entry; the other bits are the count
 constexpr float kLog2e = 1.44269504088896340736f;
 
-struct __attribute__((packed, aligned(4))) Float4 { float v[4]; };
-struct __attribute__((packed, aligned(2))) Half4 { unsigned short v[4]; };
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned short halfx4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef int intx4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 __device__ __forceinline__ float finite_max(float m) { return fminf(fmaxf(m, -FLT_MAX), FLT_MAX); }
 __device__ __forceinline__ float exp_diff(float x, float m) { return __builtin_amdgcn_exp2f((x - m) * kLog2e); }
 
-// Biases of the chunk's tokens, summed per token in the order of the list: the entries that name one of them are packed in order, and
+// x / y from r = 1 / y: the quotient's remainder corrects it, so it is off by no more than a division (what is infinite stays so).
+__device__ __forceinline__ float divided(float x, float y, float r) {
+  const float q = x * r, e = __builtin_fmaf(-q, y, x);
+  return fabsf(q) < INFINITY ? __builtin_fmaf(e, r, q) : q;
+}
+
+// Biases of the chunk's tokens, summed per token in the order of the list (its first NT entries are given): the entries that name one of them are packed in order, and
 // the first of each token adds up its like.
-__device__ void sum_biases(const EditArgs& a, int b, int c0, float* s_bias, int* s_id, float* s_val, int* s_base) {
+template <int NT>
+__device__ void sum_biases(const EditArgs& a, int b, int c0, int id0, float value0, float* s_bias, int* s_id, float* s_val, int* s_base) {
+  constexpr int NW = NT / kWave, kChunk = NT * kPer;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t* ids = a.bias_ids + (size_t)b * a.n_bias;
   const float* vals = a.bias_values + (size_t)b * a.n_bias;
   for (int t0 = 0; t0 < a.n_bias; t0 += NT) {
     const int t = t0 + tid;
-    const unsigned id = t < a.n_bias ? (unsigned)ids[t] : 0xffffffffu;
+    const unsigned id = t0 == 0 ? (unsigned)id0 : t < a.n_bias ? (unsigned)ids[t] : 0xffffffffu;
+    const float value = t0 == 0 ? value0 : t < a.n_bias ? vals[t] : 0.f;
     const bool mine = id < (unsigned)a.V && id - (unsigned)c0 < (unsigned)kChunk;
     const unsigned long long vote = __ballot(mine);
     if (lane == 0) s_base[wave] = __popcll(vote);
     __syncthreads();
     int before = __popcll(vote & ((1ull << lane) - 1)), total = 0;
+#pragma unroll
     for (int w = 0; w < NW; ++w) {
-      if (w < wave) before += s_base[w];
-      total += s_base[w];
+      const int n = s_base[w];
+      before += w < wave ? n : 0;
+      total += n;
     }
     if (mine) {
       s_id[before] = (int)id - c0;
-      s_val[before] = vals[t];
+      s_val[before] = value;
     }
     __syncthreads();
     if (tid < total) {
-      const int id0 = s_id[tid];
+      const int own = s_id[tid];
       bool first = true;
-      for (int j = 0; j < tid; ++j) first = first && s_id[j] != id0;
+      for (int j = 0; j < tid; ++j) first = first && s_id[j] != own;
       if (first) {
-        float sum = s_bias[id0];
-        for (int j = tid; j < total; ++j) sum += s_id[j] == id0 ? s_val[j] : 0.f;
-        s_bias[id0] = sum;
+        float sum = s_bias[own];
+        for (int j = tid; j < total; ++j) sum += s_id[j] == own ? s_val[j] : 0.f;
+        s_bias[own] = sum;
       }
     }
-    __syncthreads();
+    if (t0 + NT < a.n_bias) __syncthreads();
   }
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int chunks, long work) {
-  __shared__ unsigned s_cnt[kChunk];
-  __shared__ float s_bias[kChunk];
+// Workgroup: (sequence, chunk, group of `slots` slots), slots innermost; sequences from b0 on.
+template <int NT, bool BF16>
+__global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks, int slots, int groups) {
+  constexpr int NW = NT / kWave, kChunk = NT * kPer;
+  __shared__ __attribute__((aligned(16))) unsigned s_cnt[kChunk];
+  __shared__ __attribute__((aligned(16))) float s_bias[kChunk];
   __shared__ int s_id[NT];
   __shared__ float s_val[NT];
   __shared__ int s_base[NW];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const unsigned per_chunk = blockIdx.x / (unsigned)groups;
+  const int m0 = (int)(blockIdx.x - per_chunk * (unsigned)groups) * slots, m1 = min(m0 + slots, a.K);
+  const int chunk = (int)(per_chunk % (unsigned)chunks), b = b0 + (int)(per_chunk / (unsigned)chunks), c0 = chunk * kChunk;
   const bool counts = a.repetition || a.presence || a.frequency;
-  for (long w = blockIdx.x; w < work; w += gridDim.x) {
-    const int b = (int)(w / chunks), chunk = (int)(w - (long)b * chunks), c0 = chunk * kChunk;
-    __syncthreads();  // the tables of the chunk before are no longer read
-    for (int i = tid; i < kChunk; i += NT) {
-      s_cnt[i] = 0;
-      s_bias[i] = 0.f;
+  const bool whole = c0 + kChunk <= a.V;
+  const int left = a.V - c0 - tid * 4;  // tokens from this thread's first on
+
+  float x[kPer];
+  uint32_t word[kPer / 4];
+  auto fetch = [&](int m) {
+    const size_t row = (size_t)b * a.seq_stride + (size_t)m * a.slot_stride + c0;
+    const uint32_t* words =
+        a.masks ? a.allowed + ((size_t)b * a.masks + (a.masks > 1 ? m : 0)) * ((size_t)(a.V + 31) / 32) + c0 / 32 : nullptr;
+#pragma unroll
+    for (int q = 0; q < kPer / 4; ++q) {
+      const unsigned c = q * (NT * 4) + tid * 4;
+      word[q] = ~0u;
+      if (words && (whole || left > q * (NT * 4))) word[q] = words[c >> 5] >> (c & 31);
+      if (whole) {
+        if constexpr (BF16) {
+          const halfx4_any v = *reinterpret_cast<const halfx4_any*>((const unsigned short*)a.logits + row + c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[4 * q + i] = __builtin_bit_cast(float, (unsigned)v[i] << 16);
+        } else {
+          const floatx4_any v = *reinterpret_cast<const floatx4_any*>((const float*)a.logits + row + c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[4 * q + i] = v[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[4 * q + i] = -INFINITY;
+          if (left > q * (NT * 4) + i) {
+            if constexpr (BF16) x[4 * q + i] = __builtin_bit_cast(float, (unsigned)((const unsigned short*)a.logits)[row + c + i] << 16);
+            else x[4 * q + i] = ((const float*)a.logits)[row + c + i];
+          }
+        }
+      }
+    }
+  };
+  // All that the table is made of is asked for at once, in front of the logits; a list's first part stays in registers.
+  const bool history = counts && a.history_max, prefix = counts && a.prefix;
+  const bool table = history || prefix || a.n_bias;
+  const int32_t* h = a.history + (size_t)b * a.history_max;
+  const int first = history && tid * 4 + 4 <= a.history_max ? 4 : 0;  // ids of the first NT * 4 that this thread holds
+  intx4_any ids = {-1, -1, -1, -1};
+  if (first) ids = *reinterpret_cast<const intx4_any*>(h + tid * 4);
+  int bias_id = -1;
+  float bias_value = 0.f;
+  if (tid < a.n_bias) {
+    bias_id = a.bias_ids[(size_t)b * a.n_bias + tid];
+    bias_value = a.bias_values[(size_t)b * a.n_bias + tid];
+  }
+  const int len = !history ? 0 : a.history_len ? min(max(a.history_len[b], 0), a.history_max) : a.history_max;
+  const int prompt = history && a.prompt_len ? min(max(a.prompt_len[b], 0), len) : 0;
+  const float rep = a.repetition ? a.repetition[b] : 1.f, inv_rep = 1.0f / rep;
+  const float pres = a.presence ? a.presence[b] : 0.f;
+  const float freq = a.frequency ? a.frequency[b] : 0.f;
+  fetch(m0);
+
+  unsigned touched = 0;  // bit i: token i of this thread has a count or a bias
+  if (table) {
+#pragma unroll
+    for (int q = 0; q < kPer / 4; ++q) {
+      reinterpret_cast<uint4*>(s_cnt)[q * NT + tid] = make_uint4(0, 0, 0, 0);
+      reinterpret_cast<float4*>(s_bias)[q * NT + tid] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     __syncthreads();
-    if (counts && a.history_max) {
-      const int len = a.history_len ? min(max(a.history_len[b], 0), a.history_max) : a.history_max;
-      const int prompt = a.prompt_len ? min(max(a.prompt_len[b], 0), len) : 0;
-      const int32_t* h = a.history + (size_t)b * a.history_max;
-      for (int i = tid; i < len; i += NT) {
-        const unsigned at = (unsigned)h[i] - (unsigned)c0;
+    if (history) {
+      auto count = [&](int i, int id) {
+        const unsigned at = (unsigned)id - (unsigned)c0;
         if (at < (unsigned)kChunk) {
           if (i < prompt) atomicOr(&s_cnt[at], kInPrompt);
           else atomicAdd(&s_cnt[at], 1u);
         }
+      };
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (tid * 4 + e < len && first) count(tid * 4 + e, ids[e]);
+      int i0 = NT * 4;
+      if (a.history_max < i0) i0 = a.history_max / 4 * 4;  // what no thread holds four of
+      for (; i0 + 16 * NT <= len; i0 += 16 * NT) {
+        intx4_any v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const intx4_any*>(h + i0 + (j * NT + tid) * 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) count(i0 + (j * NT + tid) * 4 + e, v[j][e]);
       }
+      for (int i = i0 + tid; i < len; i += NT) count(i, h[i]);
     }
-    if (a.n_bias) sum_biases(a, b, c0, s_bias, s_id, s_val, s_base);
+    if (a.n_bias) sum_biases<NT>(a, b, c0, bias_id, bias_value, s_bias, s_id, s_val, s_base);
     __syncthreads();
-    const float rep = a.repetition ? a.repetition[b] : 1.f;
-    const float pres = a.presence ? a.presence[b] : 0.f;
-    const float freq = a.frequency ? a.frequency[b] : 0.f;
-    unsigned cnt[kPer];
-    float bias[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      cnt[i] = s_cnt[(i / 4) * (NT * 4) + tid * 4 + i % 4];
-      bias[i] = s_bias[(i / 4) * (NT * 4) + tid * 4 + i % 4];
+    for (int q = 0; q < kPer / 4; ++q) {
+      const uint4 n = reinterpret_cast<const uint4*>(s_cnt)[q * NT + tid];
+      const float4 v = reinterpret_cast<const float4*>(s_bias)[q * NT + tid];
+      touched |= (n.x || v.x != 0.f ? 1u : 0u) << (4 * q) | (n.y || v.y != 0.f ? 2u : 0u) << (4 * q) |
+                 (n.z || v.z != 0.f ? 4u : 0u) << (4 * q) | (n.w || v.w != 0.f ? 8u : 0u) << (4 * q);
     }
-    for (int m = 0; m < a.K; ++m) {
-      if (counts && a.prefix && m > 0) {
-        const unsigned at = (unsigned)a.prefix[(size_t)b * a.K + m - 1] - (unsigned)c0;
+  }
+  // From here on a thread reads and writes its own tokens' entries only.
+  auto add_prefix = [&](int m) {
+    const unsigned at = (unsigned)a.prefix[(size_t)b * a.K + m] - (unsigned)c0;
+    if (at < (unsigned)kChunk && ((at >> 2) & (NT - 1)) == (unsigned)tid) {
+      ++s_cnt[at];
+      touched |= 1u << (at / (NT * 4) * 4 + (at & 3));
+    }
+  };
+  if (prefix)
+    for (int m = 0; m < m0; ++m) add_prefix(m);
+
+  for (int m = m0; m < m1; ++m) {
+    if (__any(touched != 0)) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) cnt[i] += at == (unsigned)((i / 4) * (NT * 4) + tid * 4 + i % 4) ? 1u : 0u;
-      }
-      const uint32_t* words =
-          a.masks ? a.allowed + ((size_t)b * a.masks + (a.masks > 1 ? m : 0)) * ((size_t)(a.V + 31) / 32) : nullptr;
-      float y[kPer];
-#pragma unroll
-      for (int q = 0; q < kPer / 4; ++q) {
-        const int c = c0 + q * (NT * 4) + tid * 4;
-        const long at = (long)b * a.seq_stride + (long)m * a.slot_stride + c;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = -INFINITY;
-          if (c + i < a.V) {
-            if constexpr (BF16) x = __builtin_bit_cast(float, (unsigned)((const unsigned short*)a.logits)[at + i] << 16);
-            else x = ((const float*)a.logits)[at + i];
-          }
-          const unsigned n = cnt[4 * q + i];
-          if (counts && n) {
-            x = x > 0.f ? x / rep : x * rep;
+      for (int i = 0; i < kPer; ++i)
+        if (touched >> i & 1) {
+          const unsigned at = (i / 4) * (NT * 4) + tid * 4 + i % 4, n = s_cnt[at];
+          float z = x[i];
+          if (n) {
             const float times = (float)(n & ~kInPrompt);
-            x -= freq * times;
-            x -= times > 0.f ? pres : 0.f;
+            z = z > 0.f ? divided(z, rep, inv_rep) : z * rep;
+            z -= freq * times;
+            z -= times > 0.f ? pres : 0.f;
           }
-          if (a.n_bias) x += bias[4 * q + i];
-          x *= a.inv_tau;
-          if (c + i >= a.V || (words && !((words[(c + i) >> 5] >> ((c + i) & 31)) & 1))) x = -INFINITY;
-          if (c + i < a.V) a.out[(long)b * a.out_seq_stride + (long)m * a.out_slot_stride + c + i] = x;
-          y[4 * q + i] = x;
+          x[i] = z + s_bias[at];
         }
-      }
-      float mx = y[0];
-#pragma unroll
-      for (int i = 1; i < kPer; ++i) mx = fmaxf(mx, y[i]);
-      mx = finite_max(wave_max(mx));
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) sum += exp_diff(y[i], mx);
-      sum = wave_sum(sum);
-      if (lane == 0) a.partials[((size_t)b * a.K + m) * (size_t)(chunks * NW) + chunk * NW + wave] = make_float2(mx, sum);
     }
+    float* out = a.out + (size_t)b * a.out_seq_stride + (size_t)m * a.out_slot_stride + c0;
+    float y[kPer];
+#pragma unroll
+    for (int q = 0; q < kPer / 4; ++q) {
+      const unsigned c = q * (NT * 4) + tid * 4;
+      floatx4_any v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[4 * q + i] = v[i] = word[q] >> i & 1 ? x[4 * q + i] * a.inv_tau : -INFINITY;
+      if (whole) {
+        __builtin_nontemporal_store(v, reinterpret_cast<floatx4_any*>(out + c));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (left > q * (NT * 4) + i) out[c + i] = v[i];
+      }
+    }
+    if (m + 1 < m1) fetch(m + 1);
+    float mx = y[0];
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) mx = fmaxf(mx, y[i]);
+    mx = finite_max(wave_max(mx));
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) sum += exp_diff(y[i], mx);
+    sum = wave_sum(sum);
+    if (lane == 0) a.partials[((size_t)b * a.K + m) * (size_t)(chunks * NW) + chunk * NW + wave] = make_float2(mx, sum);
+    if (prefix) add_prefix(m);
   }
 }
 
+constexpr int kLseThreads = 256;
+
 // A wavefront per row.
-__global__ __launch_bounds__(NT) void edit_lse_kernel(EditArgs a, int nP) {
+__global__ __launch_bounds__(kLseThreads) void edit_lse_kernel(EditArgs a, int nP) {
   const int lane = threadIdx.x & 63;
-  const long r = (long)blockIdx.x * NW + (threadIdx.x >> 6);
+  const long r = (long)blockIdx.x * (kLseThreads / kWave) + (threadIdx.x >> 6);
   if (r >= (long)a.B * a.K) return;
   const float2* P = a.partials + (size_t)r * nP;
   float mx = -FLT_MAX, sm = 0.f;
@@ -177,18 +272,38 @@ __global__ __launch_bounds__(NT) void edit_lse_kernel(EditArgs a, int nP) {
 
 }  // namespace
 
-int edit_partials(int V) { return (V + kChunk - 1) / kChunk * NW; }
+// A pair per wavefront and chunk, that is per 512 tokens; room for the longest chunk.
+int edit_partials(int V) { return (V + 4095) / 4096 * 8; }
 
-hipError_t launch_edit(const EditArgs& a) {
-  const int chunks = (a.V + kChunk - 1) / kChunk;
-  const long work = (long)chunks * a.B;
-  const dim3 grid((unsigned)(work < (1L << 20) ? work : (1L << 20)));
-  if (a.bf16) hipLaunchKernelGGL(edit_kernel<true>, grid, dim3(NT), 0, a.stream, a, chunks, work);
-  else hipLaunchKernelGGL(edit_kernel<false>, grid, dim3(NT), 0, a.stream, a, chunks, work);
+template <int NT>
+static void launch_edit_of(const EditArgs& a) {
+  const int chunks = (a.V + NT * kPer - 1) / (NT * kPer);
+  const long units = (long)chunks * a.B;
+  // Slots of a chunk go to workgroups of their own until there are four per CU, as long as the history that each of them counts again is
+  // short against its logits.
+  int groups = 1;
+  while (groups < a.K && units * groups < 1024 && a.history_max <= (long)((a.K + groups - 1) / groups) * (NT * kPer / 2)) groups *= 2;
+  if (groups > a.K) groups = a.K;
+  const int slots = (a.K + groups - 1) / groups;
+  groups = (a.K + slots - 1) / slots;
+  const long most = (1L << 32) / NT - 1;  // a launch holds fewer than 2^32 threads
+  const long per = most / ((long)chunks * groups);
+  for (long b0 = 0; b0 < a.B; b0 += per) {
+    const dim3 grid((unsigned)((a.B - b0 < per ? a.B - b0 : per) * chunks * groups));
+    if (a.bf16) hipLaunchKernelGGL((edit_kernel<NT, true>), grid, dim3(NT), 0, a.stream, a, (int)b0, chunks, slots, groups);
+    else hipLaunchKernelGGL((edit_kernel<NT, false>), grid, dim3(NT), 0, a.stream, a, (int)b0, chunks, slots, groups);
+  }
   if (a.out_lse) {
     const long rows = (long)a.B * a.K;
-    hipLaunchKernelGGL(edit_lse_kernel, dim3((unsigned)((rows + NW - 1) / NW)), dim3(NT), 0, a.stream, a, chunks * NW);
+    constexpr int kRows = kLseThreads / kWave;
+    hipLaunchKernelGGL(edit_lse_kernel, dim3((unsigned)((rows + kRows - 1) / kRows)), dim3(kLseThreads), 0, a.stream, a, chunks * (NT / kWave));
   }
+}
+
+// Chunks of 4096 tokens halve what is read of the histories; below, chunks of 2048 start earlier and fill the CUs more evenly.
+hipError_t launch_edit(const EditArgs& a) {
+  if (a.history_max >= 16384 || (long)a.B * a.K * a.V >= 1L << 25) launch_edit_of<512>(a);
+  else launch_edit_of<256>(a);
   return hipGetLastError();
 }
 

@@ -25,7 +25,7 @@ def _params(**kw):
     (dict(out_seq_stride=299), "overlap"), (dict(out_seq_stride=0), "overlap"), (dict(history_max=5), "history"), (dict(n_bias=1), "bias"),
     (dict(n_bias=1, bias_ids=0x1000), "bias"), (dict(masks=1), "allowed"), (dict(prefix=0x1002), "4-byte"), (dict(masks=3, allowed=0x1001), "4-byte")])
 def test_refusals(bad, word):
-    assert fb.lib().fef_edit_logits(_params(**bad), 0x1000, 0x2000, 0x3000) == fb.FEF_ERR_INVALID_ARG
+    assert fb.lib().fef_edit_logits(ctypes.byref(_params(**bad)), 0x1000, 0x2000, 0x3000) == fb.FEF_ERR_INVALID_ARG
     assert word in fb.fef_last_error()
 
 
@@ -34,7 +34,7 @@ def test_refusals(bad, word):
     (0x1000, 0x2001, 0x3000, {}), (0x1000, 0x2000, 0x3002, {}), (0x1000, 0x1000, 0x3000, dict(dtype=fb.FEF_BF16)),
     (0x1000, 0x1000, 0x3000, dict(seq_stride=400)), (0x1000, 0x1000, 0x3000, dict(slot_stride=0))])
 def test_refused_pointers(logits, out, lse, kw):
-    assert fb.lib().fef_edit_logits(_params(**kw), logits, out, lse) == fb.FEF_ERR_INVALID_ARG
+    assert fb.lib().fef_edit_logits(ctypes.byref(_params(**kw)), logits, out, lse) == fb.FEF_ERR_INVALID_ARG
 
 
 def test_workspace():
@@ -42,7 +42,7 @@ def test_workspace():
     need = fb.lib().fef_edit_workspace_bytes(p)
     assert need > 0 and need % 256 == 0
     for bad in (dict(workspace=None), dict(workspace=0x10010), dict(workspace_bytes=need - 1)):
-        assert fb.lib().fef_edit_logits(_params(**bad), 0x1000, 0x2000, 0x3000) == fb.FEF_ERR_WORKSPACE
+        assert fb.lib().fef_edit_logits(ctypes.byref(_params(**bad)), 0x1000, 0x2000, 0x3000) == fb.FEF_ERR_WORKSPACE
     assert fb.lib().fef_edit_workspace_bytes(_params(K=0)) == 0
     assert fb.lib().fef_edit_workspace_bytes(_params(B=1 << 20, out_seq_stride=300)) >= 1 << 20
     # slots outside, sequences inside is a layout too
@@ -57,3 +57,19 @@ def test_edits_checks_types():
         fb.Edits(bias_ids=torch.zeros(1, 4, dtype=torch.int32))
     with pytest.raises(AssertionError):
         fb.Edits(prompt_len=torch.zeros(1, dtype=torch.int32))
+
+
+def test_the_packed_parameters_are_the_struct():
+    """EditLogits writes the fields in one go, in the order and alignment of fef_edit_params."""
+    names = [f[0] for f in fb.fef_edit_params._fields_]
+    values = [ctypes.sizeof(fb.fef_edit_params), *range(2, 6), 0.5, *range(11, 11 + len(names) - 6)]
+    buffer = ctypes.create_string_buffer(ctypes.sizeof(fb.fef_edit_params))
+    fb._PACK_EDIT(buffer, 0, *values)
+    p = fb.fef_edit_params.from_buffer(buffer)
+    assert [getattr(p, n) for n in names] == values
+
+
+def test_the_tensors_of_edits_are_fixed():
+    e = fb.Edits()
+    with pytest.raises(AttributeError):
+        e.history = None
