@@ -76,8 +76,9 @@ def check_accumulators_isa(verbose=True, extra_flags=()):
     no wait states behind the very multiply that wrote it: the same instruction on the same registers is forwarded, and
     the compiler issues such chains back to back; four is what the smallest tile gives), and no vector instruction
     writes a register within two wait states of a multiply that reads it (most come from LDS reads, which are waited
-    for).  This checks exactly that for each instantiation."""
+    for).  This checks exactly that for each instantiation, and the results of the 4-bit head's multiplies (check_results)."""
     check_accumulators(_assembly("head_gemm_tiled256.hip", extra_flags), verbose)
+    check_results(_assembly("mx4_head.hip", extra_flags), verbose)
 
 
 def check_accumulators(lines, verbose=True):
@@ -113,6 +114,49 @@ def check_accumulators(lines, verbose=True):
                 recent += [set()] * (int(t.split()[1]) + 1 if t.startswith("s_nop") else 1)
         if verbose:
             print(f"check_accumulators_isa: {name}: {len(mfma)} multiplies in place on {len(acc)} registers", flush=True)
+
+
+RESULT_STATES = 8  # wait states the compiler keeps behind a 16x16x32 multiply before anything but a multiply touches its result
+
+
+def check_results(lines, verbose=True):
+    """The compiler looks back from an instruction for a multiply that it has to wait for, block by block, and visits a block once: where
+    a longer way through other blocks reaches it first, the short way is not looked at, and a result is read before it is there
+    (met where multiplies stood under conditions of their own: two of four accumulation registers kept their old value).  The 4-bit head's
+    kernels have no such multiply; this walks every path of theirs and checks that none is short of wait states."""
+    kernels = [i for i, l in enumerate(lines) if re.match(r"^_Z\w*mx4_\w*kernel\w*:", l)]
+    if not kernels:
+        raise RuntimeError("check_results: no kernel in the assembly")
+    for start in kernels:
+        name = lines[start].split(":")[0]
+        code, labels = [], {}
+        for line in lines[start + 1:next(i for i in range(start, len(lines)) if lines[i].startswith(".Lfunc_end"))]:
+            t = line.split(";")[0].strip()
+            if re.match(r"^\.?[A-Za-z_][\w.$]*:", t):
+                labels[t.split(":")[0]] = len(code)
+            elif t and not t.startswith((".", "#")):
+                code.append((t.split()[0], t.split(None, 1)[1] if " " in t or "\t" in t else "", t))
+        multiplies = [i for i, c in enumerate(code) if c[0].startswith("v_mfma")]
+        if not multiplies:
+            raise RuntimeError(f"check_results: {name}: no multiply")
+        for i in multiplies:
+            result, least, ways = _regs(code[i][1].split(",")[0]), {}, [(i + 1, 0)]
+            while ways:
+                j, states = ways.pop()
+                if j >= len(code) or states >= RESULT_STATES or least.get(j, RESULT_STATES) <= states:
+                    continue
+                least[j] = states
+                op, args, text = code[j]
+                if op.startswith(("v_", "ds_", "global_", "buffer_", "flat_", "scratch_")) and not op.startswith("v_mfma") and _regs(args) & result:
+                    raise RuntimeError(f"check_results: {name}: '{text}' {states} wait states behind '{code[i][2]}'")
+                if op == "s_endpgm":
+                    continue
+                if op.startswith(("s_cbranch", "s_branch")):
+                    ways.append((labels[args.strip()], states + 1))
+                if op != "s_branch":
+                    ways.append((j + 1, states + (int(args) + 1 if op == "s_nop" else 1)))
+        if verbose:
+            print(f"check_results: {name}: {len(multiplies)} results waited for", flush=True)
 
 
 HARNESS_SRC = os.path.join(os.path.dirname(HERE), "tests", "c_abi", "abi_harness.cpp")

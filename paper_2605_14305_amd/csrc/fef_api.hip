@@ -522,7 +522,8 @@ fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* c
     return fail(FEF_ERR_INVALID_ARG, "struct_size %u does not match this library's %zu", prm->struct_size, sizeof(fef_params));
   if (R < 1 || R > (1 << 24)) return fail(FEF_ERR_INVALID_ARG, "R = %d out of range [1, 2^24]", R);
   if (prm->V < 1 || prm->d < 1) return fail(FEF_ERR_INVALID_ARG, "V and d must be positive");
-  if (prm->d % 32 != 0) return fail(FEF_ERR_INVALID_ARG, "a 4-bit head needs d to be a multiple of 32 (got %d)", prm->d);
+  if (prm->d % 32 != 0 || prm->d > (1 << 20))
+    return fail(FEF_ERR_INVALID_ARG, "a 4-bit head needs d to be a multiple of 32, at most 2^20 (got %d)", prm->d);
   if (prm->dtype != FEF_BF16 && prm->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", prm->dtype);
   if (!(prm->temperature > 0.f) || !(prm->temperature < 1e30f))
     return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number");

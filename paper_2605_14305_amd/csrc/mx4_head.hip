@@ -10,6 +10,8 @@
 // Layout.  The multiply adds over k in any order as long as both operands agree on it.  Lane l = (token or row l % 16, group g = l / 16)
 // takes the 32 codes of block 4 u + g (16 bytes and one scale), which feed four multiplies of 8 codes per lane; of h it takes the same
 // columns.  Tokens are the rows of D, so a lane ends with four consecutive tokens of one row of h.
+#include <type_traits>
+
 #include "head_common.hpp"
 
 namespace fef {
@@ -51,7 +53,6 @@ __device__ __forceinline__ void split3(const float* x, bf16x8 (&part)[3]) {
 }
 
 constexpr int kWaves = 8, kThreads = kWaves * kWave;
-constexpr int kUnit = 256;  // columns per stage of h; two of them share a load of 16 scales
 
 // 16 or 4 bytes per lane from base + offset straight to LDS, lane after lane from lds_off on; counted by hand (wait_newer).
 __device__ __forceinline__ void request_16(const void* base, uint32_t offset, uint32_t lds_off) {
@@ -62,227 +63,6 @@ __device__ __forceinline__ void request_4(const void* base, uint32_t offset, uin
 }
 
 typedef float floatx4_any __attribute__((ext_vector_type(4), aligned(4)));
-struct __attribute__((packed, aligned(1))) Bytes16 { int v[4]; };
-
-// The walk: a workgroup per CU takes a run of 16-token tiles, wavefront w the tiles w, w + 8, ... of up to 8 TT of them at a time, and walks
-// over k in stages of 256 columns.  Codes come from memory straight into the registers that the conversion reads, a ring of up to 4 KB
-// per tile ahead (the whole wait for HBM is hidden behind it); 128 bytes of a row at a time, a whole line.  h, which all wavefronts share,
-// comes through LDS in two stages, 16-byte pieces exchanged so that 16 rows meet all banks.
-// grid (runs, row blocks of 16 MT).
-template <int TT, int MT, bool F32>
-__global__ __launch_bounds__(kThreads, 2) void mx4_walk_kernel(Mx4Args a, int passes) {
-  constexpr int DS = TT >= 3 ? 1 : TT == 2 ? 2 : 4;  // pairs of stages in the ring
-  constexpr int P = F32 ? 3 : 1, ROWS = 16 * MT;
-  __shared__ bf16x8 s_h[2][P][ROWS * (kUnit / 8)];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int i16 = lane & 15, g = lane >> 4;
-  const int nb = a.d / 32, nu = (nb + 7) / 8;
-  const int tiles = (a.V + 15) / 16;
-  const int run0 = (int)((long)blockIdx.x * tiles / gridDim.x), run1 = (int)((long)(blockIdx.x + 1) * tiles / gridDim.x);
-  const int row0 = blockIdx.y * ROWS;
-  // Addresses are a scalar pointer that moves and a 32-bit offset per lane that does not, which keeps them out of the vector registers.
-  constexpr int kElem = F32 ? 4 : 2;
-  const char* h0 = (const char*)a.h + (size_t)row0 * a.d * kElem;
-
-  // h, stage u: thread -> pieces of eight columns
-  uint32_t h_off[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int item = tid + i * kThreads;
-    h_off[i] = (uint32_t)min(item >> 5, a.R - 1 - row0) * (uint32_t)a.d * kElem + (item & 31) * 8 * kElem;
-  }
-  float xf[F32 ? MT : 1][8];
-  bf16x8 xb[F32 ? 1 : MT];
-  auto fetch_h = [&](int u) {
-    const char* at = h0 + (size_t)u * kUnit * kElem;
-    const bool in = u * kUnit + (tid & 31) * 8 < a.d;
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      if constexpr (F32) {
-        floatx4 lo = {}, hi = {};
-        if (in) {
-          lo = *reinterpret_cast<const floatx4*>(at + h_off[i]);
-          hi = *reinterpret_cast<const floatx4*>(at + h_off[i] + 16);
-        }
-        *reinterpret_cast<floatx4*>(xf[i]) = lo;
-        *reinterpret_cast<floatx4*>(xf[i] + 4) = hi;
-      } else {
-        xb[i] = bf16x8{};
-        if (in) xb[i] = *reinterpret_cast<const bf16x8*>(at + h_off[i]);
-      }
-    }
-  };
-  auto store_h = [&](int buf) {
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int item = tid + i * kThreads, row = item >> 5, slot = row * 32 + ((item & 31) ^ (row & 15));
-      if constexpr (F32) {
-        bf16x8 part[3];
-        split3(xf[i], part);
-#pragma unroll
-        for (int p = 0; p < 3; ++p) s_h[buf][p][slot] = part[p];
-      } else {
-        s_h[buf][0][slot] = xb[i];
-      }
-    }
-  };
-
-  for (int pass = 0; pass < passes; ++pass) {
-    const int t0 = run0 + (int)((long)pass * (run1 - run0) / passes), t1 = run0 + (int)((long)(pass + 1) * (run1 - run0) / passes);
-    intx4 w[DS][2][TT][2];
-    intx4 sc[DS][TT];
-    const uint8_t *codes[TT], *scales[TT];
-    uint32_t code_off[TT], scale_off[TT];
-    // the runs' lengths differ by one tile at most, so a wavefront has TT of them or TT - 1
-    const bool full = t0 + wave + (TT - 1) * kWaves < t1;
-#pragma unroll
-    for (int t = 0; t < TT; ++t) {
-      const int tok0 = min(t0 + wave + t * kWaves, t1 - 1) * 16;
-      const uint32_t r = min(i16, a.V - 1 - tok0);
-      codes[t] = a.codes + (size_t)tok0 * (a.d / 2);
-      scales[t] = a.scales + (size_t)tok0 * nb;
-      code_off[t] = r * (uint32_t)(a.d / 2);
-      scale_off[t] = r * (uint32_t)nb;
-    }
-    // codes of half a pair of stages, scales of a whole one; blocks past the row: its last codes, times h = 0, with a scale of one
-    auto fetch_codes = [&](int slot, int half, int pair) {
-      const int kb = 16 * pair + 8 * half;
-      if (kb + 8 <= nb) {
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-          if (t < TT - 1 || full) {
-            const uint8_t* at = codes[t] + (size_t)kb * 16;
-            w[slot][half][t][0] = *reinterpret_cast<const intx4*>(at + (code_off[t] + g * 16));
-            w[slot][half][t][1] = *reinterpret_cast<const intx4*>(at + (code_off[t] + g * 16) + 64);
-          }
-      } else {
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-          if (t < TT - 1 || full) {
-            w[slot][half][t][0] = *reinterpret_cast<const intx4*>(codes[t] + (code_off[t] + min(kb + g, nb - 1) * 16));
-            w[slot][half][t][1] = *reinterpret_cast<const intx4*>(codes[t] + (code_off[t] + min(kb + 4 + g, nb - 1) * 16));
-          }
-      }
-    };
-    auto fetch_scales = [&](int slot, int pair) {
-      if (16 * pair + 16 <= nb) {
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-          if (t < TT - 1 || full) sc[slot][t] = __builtin_bit_cast(intx4, *reinterpret_cast<const Bytes16*>(scales[t] + 16 * pair + scale_off[t]));
-      } else {
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-          if (t < TT - 1 || full) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const int kb = 16 * pair + 4 * q + g;
-              sc[slot][t][q] = (kb < nb ? (int)scales[t][scale_off[t] + min(kb, nb - 1)] : 127) << (8 * g);
-            }
-          }
-      }
-    };
-
-    floatx4 acc[TT][MT] = {};
-    fetch_h(0);
-#pragma unroll
-    for (int s = 0; s < DS; ++s) {
-      if (2 * s < nu) {
-        fetch_scales(s, s);
-        fetch_codes(s, 0, s);
-      }
-      if (2 * s + 1 < nu) fetch_codes(s, 1, s);
-    }
-    if (pass) lds_barrier();  // the last stage of the pass before has been read
-    store_h(0);
-    lds_barrier();
-    for (int pair0 = 0; 2 * pair0 < nu; pair0 += DS) {
-#pragma unroll
-      for (int s = 0; s < DS; ++s) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int pair = pair0 + s, u = 2 * pair + half;
-          if (u < nu) {
-            if (u + 1 < nu) fetch_h(u + 1);
-            // eight multiplies' worth of columns per lane and stage; fragments of h are read one step ahead
-            bf16x8 x[2][P][MT];
-            auto read_h = [&](int step) {
-              const int piece = (16 * (step >> 2) + 4 * g + (step & 3)) ^ i16;
-#pragma unroll
-              for (int p = 0; p < P; ++p)
-#pragma unroll
-                for (int m = 0; m < MT; ++m) x[step & 1][p][m] = s_h[half][p][(16 * m + i16) * 32 + piece];
-            };
-            read_h(0);
-            float scale[TT];
-#pragma unroll
-            for (int step = 0; step < 8; ++step) {
-              if (step + 1 < 8) read_h(step + 1);
-#pragma unroll
-              for (int t = 0; t < TT; ++t)
-                if (t < TT - 1 || full) {
-                  if ((step & 3) == 0)
-                    scale[t] = __builtin_bit_cast(float, __builtin_amdgcn_ubfe((unsigned)sc[s][t][2 * half + (step >> 2)], 8 * g, 8) << 23);
-                  const bf16x8 v = unpack8(w[s][half][t][step >> 2][step & 3], scale[t]);
-#pragma unroll
-                  for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int p = P - 1; p >= 0; --p) acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, x[step & 1][p][m], acc[t][m], 0, 0, 0);
-                }
-              __builtin_amdgcn_sched_barrier(0);  // else all fragments of a stage are read at its start, into registers that the ring needs
-            }
-            if (u + 2 * DS < nu) {
-              if (half == 0) fetch_codes(s, 0, pair + DS);
-              else fetch_codes(s, 1, pair + DS);
-            }
-            if (half == 1 && u + 2 * DS - 1 < nu) fetch_scales(s, pair + DS);
-            if (u + 1 < nu) store_h(half ^ 1);
-            lds_barrier();
-          }
-        }
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        asm volatile("" : "+v"(acc[t][m]));  // the multiplies need all lanes: none may move under a condition
-        const int row = row0 + 16 * m + i16, tok = (t0 + wave + t * kWaves) * 16 + 4 * g;
-        if ((t < TT - 1 || full) && row < a.R) {
-          float* out = a.logits + (size_t)row * a.ld + tok;
-          const floatx4 y = acc[t][m] * a.inv_tau;
-          if (tok + 4 <= a.V) {
-            *reinterpret_cast<Float4*>(out) = Float4{{y[0], y[1], y[2], y[3]}};
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (tok + i < a.V) out[i] = y[i];
-          }
-        }
-      }
-  }
-}
-
-template <int TT, int MT, bool F32>
-void launch_walk(const Mx4Args& a, int runs, int passes) {
-  const dim3 grid(runs, (a.R + 16 * MT - 1) / (16 * MT));
-  FEF_LAUNCH_HEAD((mx4_walk_kernel<TT, MT, F32>), grid, dim3(kThreads), a, a, passes);
-}
-
-template <int MT, bool F32>
-void launch_walk_of(const Mx4Args& a) {
-  const int tiles = (a.V + 15) / 16, runs = tiles < 256 ? tiles : 256;
-  const int longest = (tiles + runs - 1) / runs;
-  const int passes = (longest + 8 * 5 - 1) / (8 * 5);
-  const int tt = ((longest + passes - 1) / passes + 7) / 8;
-  switch (tt) {
-    case 1: launch_walk<1, MT, F32>(a, runs, passes); break;
-    case 2: launch_walk<2, MT, F32>(a, runs, passes); break;
-    case 3: launch_walk<3, MT, F32>(a, runs, passes); break;
-    case 4: launch_walk<4, MT, F32>(a, runs, passes); break;
-    default: launch_walk<5, MT, F32>(a, runs, passes); break;
-  }
-}
-
 
 // Up to 16 MT rows whose h fits the registers.  A workgroup per CU takes a run of 16-token tiles in stages of TG of them, up to 32 KB of
 // codes and 2 KB of scales, which come in the order of memory straight into LDS, RING - 1 stages ahead.  Its eight wavefronts are KS slices of
@@ -431,26 +211,26 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_stages_kernel(Mx4Args a, int 
     intx4 w[UPW];
     int sc[UPW];
 #pragma unroll
-    for (int u = 0; u < UPW; ++u)
-      if (u < UPW - 1 || count == UPW) {
-        const int kb = min(4 * (u0 + u) + g, nb - 1);
-        w[u] = s_codes[slot][row * nb + (kb ^ (row & swap))];
-        sc[u] = 4 * (u0 + u) + g < nb ? reinterpret_cast<const uint8_t*>(s_scales[slot])[row * nb + kb] : 127;
-      }
+    for (int u = 0; u < UPW; ++u) {  // a unit that this slice lacks, and blocks past the row: some codes, times h = 0, with a scale of one
+      const int kb = min(4 * (u0 + u) + g, nb - 1), in = u < count && 4 * (u0 + u) + g < nb ? -1 : 0;
+      w[u] = s_codes[slot][row * nb + (kb ^ (row & swap))];
+      sc[u] = (reinterpret_cast<const uint8_t*>(s_scales[slot])[row * nb + kb] & in) | (127 & ~in);
+    }
     floatx4 acc[MT] = {};
 #pragma unroll
-    for (int u = 0; u < UPW; ++u)
-      if (u < UPW - 1 || count == UPW) {
-        const float scale = __builtin_bit_cast(float, sc[u] << 23);
+    for (int u = 0; u < UPW; ++u) {
+      const float scale = __builtin_bit_cast(float, sc[u] << 23);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const bf16x8 v = unpack8(w[u][q], scale);
+      for (int q = 0; q < 4; ++q) {
+        const bf16x8 v = unpack8(w[u][q], scale);
 #pragma unroll
-          for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int p = P - 1; p >= 0; --p) acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, h[u][q][p][m], acc[m], 0, 0, 0);
-        }
+          for (int p = P - 1; p >= 0; --p) acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, h[u][q][p][m], acc[m], 0, 0, 0);
       }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) asm volatile("" : "+v"(acc[m]));  // no multiply moves under a condition
     if (KS == 1) {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
@@ -490,21 +270,321 @@ bool launch_stages(const Mx4Args& a) {
   return true;
 }
 
+
+__device__ __forceinline__ void request_2(const void* base, uint32_t offset, uint32_t lds_off) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_ushort %0, %1" :: "v"(offset), "s"(base), "s"(lds_off) : "memory");
+}
+
+// More rows: a workgroup takes a run of up to WC TT tiles times 16 M WR rows through steps of 128 columns.  Its eight wavefronts are WR groups of
+// 16 M rows times WC = 8 / WR columns of tiles, wavefront column c with the tiles c, c + WC, ... of the run: codes become bf16 where they are used,
+// once for 16 M rows, and a fragment of h serves TT tiles.  All of it is requested straight into LDS: h, which L2 holds, one step ahead by
+// wavefronts 0 to 3, and whole 128-byte lines of codes, two steps at a time, up to four steps ahead by the others (requests of one
+// wavefront complete in order, so one that had asked for both would wait for the far ones with the near ones).
+template <int M, int WR, int TT, bool F32>
+__global__ __launch_bounds__(kThreads, 2) void mx4_tile_kernel(Mx4Args a, int runs, int row_blocks) {
+  constexpr int P = F32 ? 3 : 1, WC = 8 / WR, ROWS = 16 * M * WR, TOK = 16 * WC * TT, kElem = F32 ? 4 : 2;
+  constexpr int HI = (ROWS * 8 * kElem + 255) / 256, CI = TOK / 32, SI = TOK / 64;  // requests per wavefront: h per step, codes and scales per pair
+  constexpr int kH = HI * 4096, kC = TOK * 128, kS = TOK * 16, kOutLd = TOK + 4;
+  constexpr int kFit = ((160 << 10) - 2 * kH) / (kC + kS), CR = kFit < 3 ? kFit : 3;  // pairs of steps in LDS; of h: two steps
+  constexpr int kBytes = 2 * kH + CR * (kC + kS);
+  static_assert(ROWS * kOutLd * 4 <= kBytes && CR >= 2 && TOK % 64 == 0, "");
+  __shared__ __attribute__((aligned(16))) char smem[kBytes];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i16 = lane & 15, g = lane >> 4, wc = wave % WC, wr = wave / WC;
+  const int asks_codes = wave >> 2, quarter = wave & 3;
+  // Row blocks of a run go to one XCD one behind another.
+  const int q = blockIdx.x >> 3, by = q % row_blocks, bx = q / row_blocks * 8 + (blockIdx.x & 7);
+  if (bx >= runs) return;
+  const int nb = a.d / 32, steps = (nb + 3) / 4, pairs = (nb + 7) / 8;
+  const int tiles = (a.V + 15) / 16;
+  const int t0 = (int)((long)bx * tiles / runs), t1 = (int)((long)(bx + 1) * tiles / runs);
+  const int row0 = by * ROWS;
+  const int last = min(t1 * 16, a.V) - 1 - t0 * 16;                    // last token there is, from the run's first
+
+  // Where this lane's 16-byte pieces come from: request i fills the pieces (4 i + quarter) 64 + lane of its step or pair.
+  constexpr int NI = HI > CI ? HI : CI;
+  uint32_t off[NI], s_off[SI];
+  auto piece_of = [&](int i) { return (i * 4 + quarter) * kWave + lane; };
+  auto h_column = [&](int i) { const int s = piece_of(i); return (s & (8 * kElem - 1)) ^ (s / (8 * kElem) & 15); };
+  auto c_chunk = [&](int i) { const int s = piece_of(i); return (s & 7) ^ (s >> 4 & 7); };
+  if (!asks_codes) {
+#pragma unroll
+    for (int i = 0; i < HI; ++i) off[i] = (uint32_t)min(piece_of(i) / (8 * kElem), a.R - 1 - row0) * (uint32_t)a.d * kElem + h_column(i) * 16;
+  } else {
+#pragma unroll
+    for (int i = 0; i < CI; ++i) off[i] = (uint32_t)min(piece_of(i) >> 3, last) * (uint32_t)(a.d / 2) + c_chunk(i) * 16;
+  }
+#pragma unroll
+  for (int i = 0; i < SI; ++i)  // 64 words: two scales, number `quarter` of the pair's four, of 64 tokens
+    s_off[i] = (uint32_t)min(i * kWave + lane, last) * (uint32_t)nb + 2 * quarter;
+  const char* h0 = (const char*)a.h + (size_t)row0 * a.d * kElem;
+  const uint8_t* codes = a.codes + (size_t)t0 * 16 * (a.d / 2);
+  const uint8_t* scales = a.scales + (size_t)t0 * 16 * nb;
+  const uint32_t lds = lds_offset(smem);
+  // What lies past the row is taken from its end and not used.
+  auto request_h = [&](int step) {
+    const uint32_t at = lds + (step & 1) * kH + quarter * 1024;
+    const char* from = h0 + (size_t)step * 128 * kElem;
+    const bool half = 4 * step + 4 > nb;
+#pragma unroll
+    for (int i = 0; i < HI; ++i) request_16(from, off[i] - (half && h_column(i) >= 4 * kElem ? 64 * kElem : 0), at + i * 4096);
+  };
+  auto request_c = [&](int pair) {
+    const uint32_t at = lds + 2 * kH + pair % CR * (kC + kS);
+    const uint8_t *c = codes + (size_t)pair * 128, *s = scales + (size_t)pair * 8;
+    const int left = nb - 8 * pair;  // blocks of the row from the pair's first on
+    if (left >= 8) {
+#pragma unroll
+      for (int i = 0; i < CI; ++i) request_16(c, off[i], at + quarter * 1024 + i * 4096);
+#pragma unroll
+      for (int i = 0; i < SI; ++i) request_2(s, s_off[i], at + kC + quarter * (TOK * 4) + i * 256);
+    } else {
+#pragma unroll
+      for (int i = 0; i < CI; ++i) request_16(c, off[i] - max(c_chunk(i) - (left - 1), 0) * 16, at + quarter * 1024 + i * 4096);
+#pragma unroll
+      for (int i = 0; i < SI; ++i) request_2(s, s_off[i] - max(2 * quarter - (left - 2), 0), at + kC + quarter * (TOK * 4) + i * 256);
+    }
+  };
+  if (!asks_codes) {
+    request_h(0);
+  } else {
+#pragma unroll
+    for (int n = 0; n < CR - 1; ++n)
+      if (n < pairs) request_c(n);
+  }
+
+  // Fragments of eight columns per lane are read and converted under the multiplies of the eight before, the first of a step under the
+  // last of the step before: those are multiplied behind the barrier.
+  floatx4 acc[TT][M] = {};
+  bf16x8 x[2][P][M] = {}, v[2][TT] = {};
+  auto multiply = [&](int j) {
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int p = P - 1; p >= 0; --p) acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[j & 1][t], x[j & 1][p][m], acc[t][m], 0, 0, 0);
+  };
+  auto step = [&](int n, auto half) {
+    if (!asks_codes) {
+      wait_newer<0>();
+    } else if (!(n & 1)) {  // later pairs may still be under way
+      if (CR > 2 && n / 2 + 1 < pairs) wait_newer<CI + SI>();
+      else wait_newer<0>();
+    }
+    lds_barrier();
+    const bf16x8* s_h = reinterpret_cast<const bf16x8*>(smem + (n & 1) * kH);
+    const char* at = smem + 2 * kH + n / 2 % CR * (kC + kS);
+    const intx4* s_c = reinterpret_cast<const intx4*>(at);
+    const int* s_s = reinterpret_cast<const int*>(at + kC) + (2 * (n & 1) + (g >> 1)) * TOK;
+    const int keep = g < 2 ? -1 : 0;  // half a step: what its last two blocks hold is masked, without a branch in front of a multiply
+    intx4 w[TT];
+    int b[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      const int tok = (WC * t + wc) * 16 + i16;
+      w[t] = s_c[tok * 8 + ((4 * (n & 1) + g) ^ (tok >> 1 & 7))];
+      b[t] = s_s[tok];
+    }
+    floatx4 f[2][F32 ? M : 1];
+    auto read_h = [&](int j) {
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        const int row = (wr * M + m) * 16 + i16;
+        if constexpr (F32) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            f[e][m] = reinterpret_cast<const floatx4*>(s_h)[row * 32 + ((8 * g + 2 * j + e) ^ i16)];
+            if (half) f[e][m] = __builtin_bit_cast(floatx4, __builtin_bit_cast(intx4, f[e][m]) & keep);
+          }
+        } else {
+          x[j & 1][0][m] = s_h[row * 16 + ((4 * g + j) ^ i16)];
+          if (half) x[j & 1][0][m] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(intx4, x[j & 1][0][m]) & keep);
+        }
+      }
+    };
+    auto convert = [&](int j) {
+      if constexpr (F32) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          const float xs[8] = {f[0][m][0], f[0][m][1], f[0][m][2], f[0][m][3], f[1][m][0], f[1][m][1], f[1][m][2], f[1][m][3]};
+          bf16x8 part[3];
+          split3(xs, part);
+#pragma unroll
+          for (int p = 0; p < P; ++p) x[j & 1][p][m] = part[p];
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        int s = (b[t] >> (8 * (g & 1))) & 255;
+        if (half) {
+          if (j == 0) w[t] &= keep;
+          s = (s & keep) | (127 & ~keep);
+        }
+        v[j & 1][t] = unpack8(w[t][j], __builtin_bit_cast(float, s << 23));
+      }
+    };
+    read_h(0);
+    multiply(3);
+    if (!asks_codes) {
+      if (n + 1 < steps) request_h(n + 1);
+    } else if (!(n & 1) && n / 2 + CR - 1 < pairs) {
+      request_c(n / 2 + CR - 1);
+    }
+    convert(0);
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+      read_h(j + 1);
+      if constexpr (!F32) convert(j + 1);
+      multiply(j);
+      if constexpr (F32) convert(j + 1);
+    }
+  };
+  const int whole = nb / 4;
+  for (int n = 0; n < whole; ++n) step(n, std::false_type{});
+  if (whole < steps) step(whole, std::true_type{});
+  multiply(3);
+#pragma unroll
+  for (int t = 0; t < TT; ++t)
+#pragma unroll
+    for (int m = 0; m < M; ++m) asm volatile("" : "+v"(acc[t][m]));  // the multiplies need all lanes: none may move under a condition
+
+  // Logits change places in LDS and leave row by row.
+  lds_barrier();
+  float* s_out = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int t = 0; t < TT; ++t)
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+      *reinterpret_cast<floatx4*>(s_out + ((wr * M + m) * 16 + i16) * kOutLd + (WC * t + wc) * 16 + 4 * g) = acc[t][m] * a.inv_tau;
+  lds_barrier();
+  const int rows = min(ROWS, a.R - row0);
+  for (int row = wave; row < rows; row += kWaves) {
+    for (int c = lane * 4; c <= last; c += 4 * kWave) {
+      float* out = a.logits + (size_t)(row0 + row) * a.ld + t0 * 16 + c;
+      const floatx4 y = *reinterpret_cast<const floatx4*>(s_out + row * kOutLd + c);
+      if (c + 3 <= last) {
+        __builtin_nontemporal_store(y, reinterpret_cast<floatx4_any*>(out));
+      } else {
+        for (int i = 0; c + i <= last; ++i) out[i] = y[i];
+      }
+    }
+  }
+}
+
+template <int M, int WR, bool F32>
+void launch_tile(const Mx4Args& a) {
+  constexpr int ROWS = 16 * M * WR, WC = 8 / WR, kMostTT = WR == 1 ? 3 : 4;
+  const int row_blocks = (a.R + ROWS - 1) / ROWS;
+  const long tiles = (a.V + 15) / 16, least = (tiles + WC * kMostTT - 1) / (WC * kMostTT);
+  // As many runs as fill whole rounds of one workgroup per CU.
+  const long rounds = (least * row_blocks + 255) / 256;
+  long runs = rounds * 256 / row_blocks;
+  if (runs < least) runs = least;
+  if (runs > tiles) runs = tiles;
+  const dim3 grid((unsigned)((runs + 7) / 8 * 8 * row_blocks));
+  const int tt = (int)((tiles + runs - 1) / runs + WC - 1) / WC;
+#define MX4_TILE(n) case n: FEF_LAUNCH_HEAD((mx4_tile_kernel<M, WR, n, F32>), grid, dim3(kThreads), a, a, (int)runs, row_blocks); break
+  switch (tt) {
+    MX4_TILE(1);
+    MX4_TILE(2);
+    default:
+      if constexpr (kMostTT > 2) {
+        switch (tt) {
+          MX4_TILE(3);
+          default:
+            if constexpr (kMostTT > 3) switch (tt) { MX4_TILE(4); }
+        }
+      }
+  }
+#undef MX4_TILE
+}
+
+constexpr int kRowsPerWave = 64;
+
+// Rows of d = 32 (2 n + 1), which are no whole pairs of blocks: a wavefront per 16 tokens and 64 rows, straight from memory; grid (groups of 64 tokens, groups of 64 rows).
+template <bool F32>
+__global__ __launch_bounds__(256) void mx4_kernel(Mx4Args a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i16 = lane & 15, g = lane >> 4;
+  const int nb = a.d / 32;  // blocks of 32 codes per row
+  const int tok0 = (blockIdx.x * 4 + wave) * 16;
+  if (tok0 >= a.V) return;
+  const int tok = min(tok0 + i16, a.V - 1);
+  const uint8_t* codes = a.codes + (size_t)tok * (a.d / 2);
+  const uint8_t* scales = a.scales + (size_t)tok * nb;
+  for (int row0 = blockIdx.y * kRowsPerWave; row0 < a.R; row0 += gridDim.y * kRowsPerWave) {
+    floatx4 acc[4] = {};
+    for (int u = 0; u < (nb + 3) / 4; ++u) {
+      const int kb = 4 * u + g;
+      const bool in = kb < nb;
+      const intx4 c = in ? *reinterpret_cast<const intx4*>(codes + kb * 16) : intx4{0, 0, 0, 0};
+      const float s = __builtin_bit_cast(float, (in ? (int)scales[kb] : 127) << 23);
+      bf16x8 w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = unpack8(c[j], s);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = min(row0 + 16 * q + i16, a.R - 1);
+        const size_t at = (size_t)row * a.d + (size_t)kb * 32;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (F32) {
+            float x[8] = {};
+            if (in) {
+              *reinterpret_cast<floatx4*>(x) = *reinterpret_cast<const floatx4*>((const float*)a.h + at + 8 * j);
+              *reinterpret_cast<floatx4*>(x + 4) = *reinterpret_cast<const floatx4*>((const float*)a.h + at + 8 * j + 4);
+            }
+            bf16x8 part[3];
+            split3(x, part);
+#pragma unroll
+            for (int p = 2; p >= 0; --p) acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j], part[p], acc[q], 0, 0, 0);
+          } else {
+            bf16x8 x = {};
+            if (in) x = *reinterpret_cast<const bf16x8*>((const __bf16*)a.h + at + 8 * j);
+            acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j], x, acc[q], 0, 0, 0);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) asm volatile("" : "+v"(acc[q]));  // the multiplies need all lanes: none may move under a condition
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int row = row0 + 16 * q + i16;
+      if (row >= a.R) continue;
+      float* out = a.logits + (size_t)row * a.ld;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (tok0 + 4 * g + i < a.V) out[tok0 + 4 * g + i] = acc[q][i] * a.inv_tau;
+    }
+  }
+}
+
 }  // namespace
 
 hipError_t launch_mx4(const Mx4Args& a) {
-  if (a.f32) {
-    if (a.R <= 16 && launch_stages<1, true>(a)) {}
-    else if (a.R <= 16) launch_walk_of<1, true>(a);
-    else launch_walk_of<2, true>(a);
-  } else {
-    if (a.R <= 16 && launch_stages<1, false>(a)) {}
-    else if (a.R <= 32 && launch_stages<2, false>(a)) {}
-    else if (a.R <= 16) launch_walk_of<1, false>(a);
-    else if (a.R <= 32) launch_walk_of<2, false>(a);
-    else if (a.R <= 48) launch_walk_of<3, false>(a);
-    else launch_walk_of<4, false>(a);
+  if (a.d % 64 == 0) {
+    if (a.f32) {
+      if (a.R <= 16 && launch_stages<1, true>(a)) return hipGetLastError();
+      if (a.R <= 32) launch_tile<1, 2, true>(a);
+      else launch_tile<2, 2, true>(a);
+    } else {
+      if (a.R <= 16 && launch_stages<1, false>(a)) return hipGetLastError();
+      if (a.R <= 32 && launch_stages<2, false>(a)) return hipGetLastError();
+      const int blocks = (a.R + 127) / 128, rows = (a.R + blocks - 1) / blocks;
+      if (rows <= 32) launch_tile<2, 1, false>(a);
+      else if (rows <= 48) launch_tile<3, 1, false>(a);
+      else if (rows <= 64) launch_tile<4, 1, false>(a);
+      else if (rows <= 96) launch_tile<3, 2, false>(a);
+      else launch_tile<4, 2, false>(a);
+    }
+    return hipGetLastError();
   }
+  const int groups = (a.R + kRowsPerWave - 1) / kRowsPerWave;
+  const dim3 grid((a.V + 63) / 64, groups < 1024 ? groups : 1024);
+  if (a.f32) FEF_LAUNCH_HEAD(mx4_kernel<true>, grid, dim3(256), a, a);
+  else FEF_LAUNCH_HEAD(mx4_kernel<false>, grid, dim3(256), a, a);
   return hipGetLastError();
 }
 

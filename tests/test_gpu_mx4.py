@@ -43,7 +43,10 @@ def _check(got, h, w, tau, dtype):
 SIZES = [(1, 32, 1), (1, 64, 17), (1, 512, 5000), (2, 96, 33), (3, 160, 130), (7, 1088, 1000), (8, 4096, 3001), (15, 2560, 777), (16, 128, 4096),
          (17, 576, 515), (31, 1024, 2049), (32, 3584, 1030), (33, 224, 999), (48, 512, 640), (55, 2560, 1003), (64, 1024, 1025), (65, 320, 300),
          (96, 64, 2000), (100, 192, 257), (128, 2048, 515), (129, 256, 800), (200, 1280, 333), (256, 512, 1024), (257, 128, 700), (300, 416, 520),
-         (512, 640, 770)]
+         (512, 640, 770),
+         # runs of every number of tiles per wavefront (some of a round of workgroups are one tile shorter), steps that end in the middle of a pair
+         (33, 128, 9000), (40, 192, 20000), (50, 384, 33000), (64, 576, 41003), (70, 64, 17000), (90, 448, 66000), (110, 320, 35001), (128, 704, 40000),
+         (20, 64, 50001), (24, 4160, 600), (3, 4224, 333)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -18,7 +18,7 @@ def _call(h=0x1000, codes=0x1000, scales=0x1000, out=0x1000, R=4, ld=1000, **par
 
 @pytest.mark.parametrize("bad,word", [
     (dict(struct_size=8), "struct_size"), (dict(R=0), "R ="), (dict(R=(1 << 24) + 1), "R ="), (dict(V=0, ld=1), "positive"),
-    (dict(d=0), "positive"), (dict(d=48), "32"), (dict(d=-32), "positive"), (dict(dtype=2), "dtype"), (dict(temperature=0.0), "temperature"),
+    (dict(d=0), "positive"), (dict(d=48), "32"), (dict(d=(1 << 20) + 32), "32"), (dict(d=-32), "positive"), (dict(dtype=2), "dtype"), (dict(temperature=0.0), "temperature"),
     (dict(temperature=float("nan")), "temperature"), (dict(temperature=float("inf")), "temperature"), (dict(h=None), "NULL"),
     (dict(codes=None), "NULL"), (dict(scales=None), "NULL"), (dict(out=None), "NULL"), (dict(h=0x1008), "16-byte"),
     (dict(codes=0x1001), "16-byte"), (dict(scales=0x1004), "16-byte"), (dict(out=0x1002), "4-byte"), (dict(ld=999), "ld"),
