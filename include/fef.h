@@ -322,6 +322,20 @@ size_t fef_edit_workspace_bytes(const fef_edit_params* prm);
  * Conventions and error behaviour as in fef_verify_step. */
 fef_status fef_edit_logits(const fef_edit_params* prm, const void* logits, float* out, float* out_lse);
 
+/* One speculative round on logits that the caller has: edited ones (fef_edit_logits), a draft half from a 4-bit head
+ * (fef_mx4_logits), or any other.  The laws are softmax(logits), draft rows first; everything else is as in fef_verify_step, phases
+ * and options included.  In the method's order a DRAFT call draws the tokens from the draft rows, the caller makes the target rows (whose
+ * edits know the drafts as their prefix), and a TARGET call verifies; the draft rows stay as they were in between.
+ *   logits  [2, B, K, ld] device float, 16-byte aligned, ld a multiple of 64 and at least V: draft rows, then target rows, already
+ *           divided by the temperature.  -inf marks a token that a law does not have; columns from V on are read but ignored.  A row
+ *           of nothing but -inf is no law: a slot with such a row is rejected (the greedy variant takes the row for token 0), and
+ *           its token, in [0, V) and with a confidence that may be NaN, means nothing
+ * Fields of prm that are read: as in fef_verify_step but for d, dtype, temperature, gemm_variant; ev_head_begin and ev_head_end
+ * must be NULL.  Workspace: fef_verify_logits_workspace_bytes (0 if the arguments are invalid). */
+size_t fef_verify_logits_workspace_bytes(const fef_params* prm, int32_t K, int32_t block);
+fef_status fef_verify_logits(const fef_params* prm, const float* logits, int64_t ld, int32_t K, int32_t block, uint64_t seed,
+                             int32_t* out_tokens, int32_t* out_accept_len, uint8_t* out_remask);
+
 /* Philox4x32-10 word 0 -> uniform, evaluated on the host with the same code the kernels
  * use; lets callers and tests reproduce a draw.  Pure host function. */
 float fef_uniform(uint64_t seed, uint32_t position, uint32_t step, uint32_t sequence,

@@ -27,7 +27,8 @@ ABI_VERSION = 11   # FEF_ABI_VERSION of include/fef.h this binding's fef_params 
 EXPORTS = ["fef_workspace_bytes", "fef_verify_step", "fef_select_gemm", "fef_uniform",
            "fef_status_string", "fef_last_error", "fef_abi_version", "fef_copy_probe", "fef_read_probe",
            "fef_cross_entropy_workspace_bytes", "fef_head_cross_entropy", "fef_topn_step",
-           "fef_verify_step_static", "fef_mx4_logits", "fef_edit_workspace_bytes", "fef_edit_logits"]
+           "fef_verify_step_static", "fef_mx4_logits", "fef_edit_workspace_bytes", "fef_edit_logits",
+           "fef_verify_logits_workspace_bytes", "fef_verify_logits"]
 FEF_STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -134,6 +135,11 @@ def lib():
         L.fef_mx4_logits.restype = ctypes.c_int
         L.fef_mx4_logits.argtypes = [ctypes.POINTER(fef_params), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                      ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64]
+        L.fef_verify_logits_workspace_bytes.restype = ctypes.c_size_t
+        L.fef_verify_logits_workspace_bytes.argtypes = [ctypes.POINTER(fef_params), ctypes.c_int32, ctypes.c_int32]
+        L.fef_verify_logits.restype = ctypes.c_int
+        L.fef_verify_logits.argtypes = [ctypes.POINTER(fef_params), ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                        ctypes.c_uint64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
         L.fef_edit_workspace_bytes.restype = ctypes.c_size_t
         L.fef_edit_workspace_bytes.argtypes = [ctypes.POINTER(fef_edit_params)]
         L.fef_edit_logits.restype = ctypes.c_int
@@ -496,3 +502,59 @@ class EditLogits:
         if r != FEF_OK:
             raise FefError(r, fef_last_error())
         return out, self.out_lse
+
+
+class VerifyLogits:
+    """The speculative round on logits that the program has (fef_verify_logits).  Holds the logits of one shape, [2, B, K, ld] with
+    the draft rows first: `draft_logits` and `target_logits` are the two [B, K, V] views that Mx4Logits and EditLogits can write
+    into.  `diag=True` also returns draft tokens, alpha, residual mass, lse and confidences."""
+
+    def __init__(self, B, K, block, V, device="cuda", diag=False):
+        self.B, self.K, self.block, self.V, self.device = B, K, block, V, torch.device(device)
+        dev = self.device
+        self.ld = (V + 63) // 64 * 64
+        self.logits = torch.zeros(2, B, K, self.ld, dtype=torch.float32, device=dev)
+        self.draft_logits, self.target_logits = self.logits[0, :, :, :V], self.logits[1, :, :, :V]
+        self.out_tokens = torch.empty(B, K, dtype=torch.int32, device=dev)
+        self.out_accept_len = torch.empty(B, dtype=torch.int32, device=dev)
+        self.out_remask = torch.empty(B, block, dtype=torch.uint8, device=dev)
+        self.diag = {}
+        if diag:
+            self.diag = {
+                "draft_tokens": torch.empty(B, K, dtype=torch.int32, device=dev),
+                "alpha": torch.empty(B, K, dtype=torch.float32, device=dev),
+                "resid_mass": torch.empty(B, K, dtype=torch.float32, device=dev),
+                "lse": torch.empty(2, B, K, dtype=torch.float32, device=dev),
+                "conf_tok": torch.empty(B, K, dtype=torch.float32, device=dev),
+            }
+        p = self._params()
+        n = lib().fef_verify_logits_workspace_bytes(ctypes.byref(p), K, block)
+        if n == 0:
+            raise FefError(FEF_ERR_INVALID_ARG, fef_last_error())
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)
+
+    def _params(self, **kw):
+        p = make_params(self.B, 64, self.V, **kw)
+        for name, t in self.diag.items():
+            setattr(p, "diag_" + name, t.data_ptr())
+        return p
+
+    def __call__(self, seed, *, step=0, seq_base=0, pos_base=0, n_rm=-1, final_pass=False, lowconf_scope=0, mask_in=None,
+                 pass_mask=None, conf=None, draft_tokens=None, n_pass=0, seq_pass=None, seq_rounds=None, tokens_state=None,
+                 phase=FEF_PHASE_FUSED, recorrupt_prob=1.0, greedy=False):
+        B, K, block = self.B, self.K, self.block
+        p = self._params(step=step, seq_base=seq_base, pos_base=pos_base, n_rm=n_rm, final_pass=final_pass, lowconf_scope=lowconf_scope)
+        for name, t, dt, shape in (("mask_in", mask_in, torch.uint8, (B, block)), ("pass_mask", pass_mask, torch.uint8, (B, block)),
+                                   ("conf", conf, torch.float32, (B, block)), ("draft_tokens", draft_tokens, torch.int32, (B, K)),
+                                   ("seq_pass", seq_pass, torch.int32, (B,)), ("seq_rounds", seq_rounds, torch.int32, (B,)),
+                                   ("tokens_state", tokens_state, torch.int32, (B, block))):
+            if t is not None:
+                assert t.dtype == dt and t.shape == shape and t.is_contiguous() and t.is_cuda
+                setattr(p, name, t.data_ptr())
+        p.n_pass, p.phase, p.recorrupt_prob, p.greedy = n_pass, phase, recorrupt_prob, int(greedy)
+        p.workspace, p.workspace_bytes, p.stream = self.workspace.data_ptr(), self.workspace.numel(), _stream(self.device)
+        s = lib().fef_verify_logits(ctypes.byref(p), _ptr(self.logits), self.ld, K, block, seed & 0xFFFFFFFFFFFFFFFF,
+                                    _ptr(self.out_tokens), _ptr(self.out_accept_len), _ptr(self.out_remask))
+        if s != FEF_OK:
+            raise FefError(s, fef_last_error())
+        return self.out_tokens, self.out_accept_len, self.out_remask

@@ -160,6 +160,14 @@ fef_status make_layout(const fef_params* p, int32_t K, int32_t block, Layout* L)
   return FEF_OK;
 }
 
+// The workspace of a call that brings its logits: all but the first area.
+void drop_logits(Layout* L) {
+  const size_t less = L->off_partials;
+  for (size_t* o : {&L->off_partials, &L->off_lse, &L->off_xdraft, &L->off_xtarget, &L->off_slot_pos, &L->off_window, &L->off_seqstate,
+                    &L->off_rmass, &L->off_amass, &L->total})
+    *o -= less;
+}
+
 __global__ __launch_bounds__(256) void copy_probe_kernel(uint4* __restrict__ dst, const uint4* __restrict__ src,
                                                         size_t n16) {
   for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < n16; i += (size_t)gridDim.x * blockDim.x)
@@ -260,7 +268,8 @@ namespace {
 constexpr int kPhaseTopN = 3;  // internal: draft rows only, then the baseline's top-n selection
 fef_status run_step(const fef_params* prm, int phase, int n_transfer, const void* h_draft, const void* h_target,
                     const void* W_vocab, int32_t K, int32_t block, uint64_t seed, int32_t* out_tokens,
-                    int32_t* out_accept_len, uint8_t* out_remask, void* workspace, size_t workspace_bytes);
+                    int32_t* out_accept_len, uint8_t* out_remask, void* workspace, size_t workspace_bytes,
+                    const float* given = nullptr, long given_ld = 0);
 }  // namespace
 
 fef_status fef_verify_step(const fef_params* prm, const void* h_draft, const void* h_target,
@@ -327,11 +336,14 @@ fef_status fef_topn_step(const fef_params* prm, const void* h, const void* W_voc
 namespace {
 fef_status run_step(const fef_params* prm, int phase, int n_transfer, const void* h_draft, const void* h_target,
                     const void* W_vocab, int32_t K, int32_t block, uint64_t seed, int32_t* out_tokens,
-                    int32_t* out_accept_len, uint8_t* out_remask, void* workspace, size_t workspace_bytes) {
+                    int32_t* out_accept_len, uint8_t* out_remask, void* workspace, size_t workspace_bytes,
+                    const float* given, long given_ld) {
   Layout L;
   fef_status s = make_layout(prm, K, block, &L);
   if (s != FEF_OK) return s;
-  if ((!h_draft && phase != FEF_PHASE_TARGET) || (!h_target && phase != FEF_PHASE_DRAFT && phase != kPhaseTopN) ||
+  if (given) {
+    drop_logits(&L);
+  } else if ((!h_draft && phase != FEF_PHASE_TARGET) || (!h_target && phase != FEF_PHASE_DRAFT && phase != kPhaseTopN) ||
       !W_vocab)
     return fail(FEF_ERR_INVALID_ARG, "h_draft, h_target and W_vocab must not be NULL");
   if (!out_tokens || ((!out_accept_len || !out_remask) && phase != FEF_PHASE_DRAFT))
@@ -362,7 +374,7 @@ fef_status run_step(const fef_params* prm, int phase, int n_transfer, const void
   memset(&v, 0, sizeof v);
   v.B = prm->B; v.K = K; v.block = block; v.V = prm->V;
   v.row0 = h.row0; v.nrows = h.nrows; v.phase = phase;
-  v.ldl = L.ldl; v.logits = (float*)(ws + L.off_logits); v.partials = (float2*)(ws + L.off_partials); v.nT = L.nT;
+  v.ldl = given ? given_ld : L.ldl; v.logits = given ? given : (float*)(ws + L.off_logits); v.partials = (float2*)(ws + L.off_partials); v.nT = L.nT;
   v.tile_unit = L.tile_unit; v.tile_T = L.tile_T; v.tile_G = L.nT;
   v.seed = seed; v.step = prm->step; v.seq_base = prm->seq_base; v.pos_base = prm->pos_base;
   v.n_rm = prm->n_rm; v.final_pass = prm->final_pass; v.lowconf_scope = prm->lowconf_scope;
@@ -388,6 +400,13 @@ fef_status run_step(const fef_params* prm, int phase, int n_transfer, const void
   v.stream = stream;
   v.n_transfer = n_transfer;
   // (events mark the head kernel alone; the masses of every slot and the logits come from kernels of their own)
+  if (given) {
+    hipError_t e = fef::launch_logit_partials(v);
+    if (e != hipSuccess) return fail(FEF_ERR_HIP, "logit kernel launch: %s", hipGetErrorString(e));
+    e = fef::launch_verify(v);
+    if (e != hipSuccess) return fail(FEF_ERR_HIP, "verify kernel launch: %s", hipGetErrorString(e));
+    return FEF_OK;
+  }
   if (L.variant == FEF_GEMM_F32 && phase == FEF_PHASE_FUSED && !h.ev_begin && !v.all_slots && !v.diag_logits &&
       fef::toy_round_serves(v.B, K, h.d, h.V)) {
     const hipError_t e = fef::launch_toy_round(h, v);
@@ -513,6 +532,38 @@ fef_status fef_head_cross_entropy(const fef_params* prm, const void* h, const vo
   e = fef::launch_ce_finish(c);
   if (e != hipSuccess) return fail(FEF_ERR_HIP, "cross-entropy kernel launch: %s", hipGetErrorString(e));
   return FEF_OK;
+}
+
+namespace {
+// A call on given logits as one of a 256-token head: a partial per tile, whatever made the logits.
+fef_status logits_params(const fef_params* prm, fef_params* p) {
+  if (!prm) return fail(FEF_ERR_INVALID_ARG, "params is NULL");
+  if (prm->struct_size != sizeof(fef_params))
+    return fail(FEF_ERR_INVALID_ARG, "struct_size %u does not match this library's %zu", prm->struct_size, sizeof(fef_params));
+  *p = *prm;
+  p->d = 64; p->dtype = FEF_BF16; p->gemm_variant = FEF_GEMM_TILED256; p->temperature = 1.f;
+  return FEF_OK;
+}
+}  // namespace
+
+size_t fef_verify_logits_workspace_bytes(const fef_params* prm, int32_t K, int32_t block) {
+  fef_params p;
+  Layout L;
+  if (logits_params(prm, &p) != FEF_OK || make_layout(&p, K, block, &L) != FEF_OK) return 0;
+  drop_logits(&L);
+  return L.total;
+}
+
+fef_status fef_verify_logits(const fef_params* prm, const float* logits, int64_t ld, int32_t K, int32_t block, uint64_t seed,
+                             int32_t* out_tokens, int32_t* out_accept_len, uint8_t* out_remask) {
+  fef_params p;
+  fef_status s = logits_params(prm, &p);
+  if (s != FEF_OK) return s;
+  if (!logits || ((uintptr_t)logits & 15)) return fail(FEF_ERR_INVALID_ARG, "logits must not be NULL and be 16-byte aligned");
+  if (ld < p.V || ld % 64 != 0 || ld > (1L << 40)) return fail(FEF_ERR_INVALID_ARG, "ld = %ld must be a multiple of 64 in [V, 2^40]", (long)ld);
+  if (p.ev_head_begin || p.ev_head_end) return fail(FEF_ERR_INVALID_ARG, "no head kernel runs in this call: ev_head_begin and ev_head_end must be NULL");
+  return run_step(&p, p.phase, 0, nullptr, nullptr, nullptr, K, block, seed, out_tokens, out_accept_len, out_remask, p.workspace,
+                  p.workspace_bytes, logits, ld);
 }
 
 fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* codes, const uint8_t* scales, int32_t R,

@@ -142,6 +142,7 @@ struct VerifyArgs {
   hipStream_t stream;
 };
 
+hipError_t launch_logit_partials(const VerifyArgs& a);  // of logits that no head kernel of this call made
 hipError_t launch_verify(const VerifyArgs& a);
 bool toy_round_serves(int B, int K, int d, int V);
 hipError_t launch_toy_round(const HeadArgs& h, const VerifyArgs& a);  // head and verify step in one launch

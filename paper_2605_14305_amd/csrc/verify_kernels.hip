@@ -525,6 +525,32 @@ __global__ __launch_bounds__(kSumThreads) void row_sums_draft_kernel(VerifyArgs 
 }
 
 // ---------------------------------------------------------------------------------------------
+// In front of kernel 1 where the caller brings the logits: (max, sum exp) of each row's 256-token tiles, a wavefront per tile, four
+// tokens per lane.  Bound: one read of the logits.
+// ---------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(NT) void logit_partials_kernel(VerifyArgs a, int row, int groups) {
+  constexpr float kLog2e = 1.4426950408889634f;
+  const int lane = threadIdx.x & 63;
+  const unsigned r = blockIdx.x / (unsigned)groups;
+  const int t = (int)(blockIdx.x - r * (unsigned)groups) * NW + (threadIdx.x >> 6);
+  if (t >= a.nT) return;
+  const int v = t * kTiled256Tn + 4 * lane;
+  floatx4 l = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  if (v < a.V) {  // rows are padded to 64 tokens
+    l = *reinterpret_cast<const floatx4*>(a.logits + (size_t)(row + r) * a.ldl + v);
+#pragma unroll
+    for (int j = 1; j < 4; ++j)
+      if (v + j >= a.V) l[j] = -INFINITY;
+  }
+  const float mx = wave_max(fmaxf(fmaxf(fmaxf(fmaxf(l[0], l[1]), l[2]), l[3]), kLowest));
+  float e = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) e += __builtin_amdgcn_exp2f((l[j] - mx) * kLog2e);
+  e = wave_sum(e);
+  if (lane == 0) const_cast<float2*>(a.partials)[(size_t)(row + r) * a.nT + t] = make_float2(mx, e);
+}
+
+// ---------------------------------------------------------------------------------------------
 // Final phase for one sequence (one workgroup): residual sample, commit, mask update, LowConf.
 // ---------------------------------------------------------------------------------------------
 
@@ -641,6 +667,7 @@ __device__ void finalize_sequence(const VerifyArgs& a, int b, const SeqState& st
           }
           const float gbest = wave_max(best);
           zz = wave_min_int(best == gbest ? bi : INT_MAX);
+          if (zz == INT_MAX) zz = 0;  // no logit above -inf
           zc = expf(Lp[zz] - lse_p);
         }
         if (tid == 0) { tmp.bcast_i = zz; tmp.bcast_f = zc; }
@@ -679,6 +706,7 @@ __device__ void finalize_sequence(const VerifyArgs& a, int b, const SeqState& st
       }
       const float gbest = block_max(best, tmp);
       z = block_min_int(best == gbest ? bi : INT_MAX, tmp);
+      if (z == INT_MAX) z = 0;  // no logit above -inf
     }
     z_conf = expf(Lp[z] - lse_p);
     }
@@ -774,11 +802,12 @@ __device__ inline void accept_tests(const VerifyArgs& a, int b, SeqState& st) {
   if (lane < window) {
     const float lq = a.logits[(size_t)sl * a.ldl + x] - lse_q;
     const float lp = a.logits[(size_t)(BK + sl) * a.ldl + x] - lse_p;
-    const float ratio = fminf(1.f, expf(lp - lq));
+    const float ratio = expf(lp - lq);
     const float u = philox_uniform(a.seed, a.pos_base + (uint32_t)pos, a.step,
                                    a.seq_base + (uint32_t)b, kStreamAccept);
     // greedy: the ratio of the two point masses is 1 if the arg maxes agree, else 0
-    rejected = a.greedy ? x != xt : !(u <= ratio);
+    // (u < 1, so this is u <= min(1, ratio); a row without a law makes the ratio NaN, which is a rejection)
+    rejected = a.greedy ? x != xt : !(ratio >= 1.f || u <= ratio);
     st.x[lane] = x;
     st.ptok[lane] = expf(lp);
   }
@@ -1171,6 +1200,16 @@ bool toy_round_serves(int B, int K, int d, int V) { return B <= 256 && 2 * K <= 
 hipError_t launch_toy_round(const HeadArgs& h, const VerifyArgs& a) {
   if (h.d % 4 == 0) hipLaunchKernelGGL(toy_round_kernel<4>, dim3(a.B), dim3(kToyWaves * kWave), 0, a.stream, h, a);
   else hipLaunchKernelGGL(toy_round_kernel<1>, dim3(a.B), dim3(kToyWaves * kWave), 0, a.stream, h, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_logit_partials(const VerifyArgs& a) {
+  const int groups = (a.nT + NW - 1) / NW;
+  const long most = ((1L << 32) / NT - 1) / groups;  // rows of a launch of fewer than 2^32 threads
+  for (long r0 = 0; r0 < a.nrows; r0 += most) {
+    const long rows = a.nrows - r0 < most ? a.nrows - r0 : most;
+    hipLaunchKernelGGL(logit_partials_kernel, dim3((unsigned)(rows * groups)), dim3(NT), 0, a.stream, a, a.row0 + (int)r0, groups);
+  }
   return hipGetLastError();
 }
 
