@@ -1,14 +1,20 @@
 // Edits of logits between a head and the token law: penalties for tokens that occurred, biases, grammar masks, and the row's
 // log-sum-exp beside the edited logits.
 //
-//   edit_kernel      a workgroup takes a chunk of kChunk tokens of one sequence through all its slots.  It counts the sequence's
-//                    history and sums its biases for these tokens in LDS, holds both per token in registers, and per slot reads the
-//                    logits once, writes them once and leaves a (max, sum exp) pair per wavefront.  Slot m + 1 differs from slot m by
-//                    one token of the prefix, which is added to the table on the way.
+//   edit_kernel      a workgroup takes a chunk of tokens of one sequence through some of its slots.  It counts the sequence's history and
+//                    sums its biases for these tokens in LDS; from then on a thread reads and writes the entries of its own tokens only,
+//                    so nothing waits: slot m + 1 differs from slot m by one token of the prefix, which that token's owner adds.  Per slot
+//                    the logits are read once, written once, and leave a (max, sum exp) pair per wavefront.  A bit per token says
+//                    whether it has an entry; the others see a multiplication and the mask.
 //   edit_lse_kernel  a wavefront per row merges the pairs.
 //
 // Counts are whole numbers, and a token's biases are added in the order of their list, so nothing depends on the order in which
 // threads arrive.
+//
+// Bound: the read and the write of the logits (32 x 16 slots of V = 151936, 622 MB: 131 us without any edit, 4.7 TB/s, a plain copy of as
+// much 121 to 130; with penalties, biases and masks 148, the edits' instructions), in small calls the way through the tables and the
+// second launch (8 slots of V = 126464: 7.6 and 2 us).  Counting the history again for every chunk beats a table in memory, which would have to
+// be cleared and needs atomics across XCDs.  Stores are non-temporal: grammar masks alone on 128 rows of V = 126464 37 -> 28 us.
 //
 // Log-sum-exp.  Maxima are clamped to the finite numbers, m in [-FLT_MAX, FLT_MAX], and differences x - m are taken before anything is
 // multiplied: a row of nothing but -inf sums to 0 and ends at -inf, one of the type's lowest value keeps it, +inf gives +inf, NaN NaN.
@@ -17,11 +23,9 @@
 #include "fef_device.hpp"
 #include "wave_ops.hpp"
 
-
 namespace fef {
 namespace {
 
-constexpr int kPer = 8;                   // tokens per thread: two runs of four
 constexpr unsigned kInPrompt = 1u << 31;  // of a table entry; the other bits are the count
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -41,7 +45,7 @@ __device__ __forceinline__ float divided(float x, float y, float r) {
 
 // Biases of the chunk's tokens, summed per token in the order of the list (its first NT entries are given): the entries that name one of them are packed in order, and
 // the first of each token adds up its like.
-template <int NT>
+template <int NT, int kPer>
 __device__ void sum_biases(const EditArgs& a, int b, int c0, int id0, float value0, float* s_bias, int* s_id, float* s_val, int* s_base) {
   constexpr int NW = NT / kWave, kChunk = NT * kPer;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -82,7 +86,7 @@ __device__ void sum_biases(const EditArgs& a, int b, int c0, int id0, float valu
 }
 
 // Workgroup: (sequence, chunk, group of `slots` slots), slots innermost; sequences from b0 on.
-template <int NT, bool BF16>
+template <int NT, int kPer, bool BF16>
 __global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks, int slots, int groups) {
   constexpr int NW = NT / kWave, kChunk = NT * kPer;
   __shared__ __attribute__((aligned(16))) unsigned s_cnt[kChunk];
@@ -183,7 +187,7 @@ __global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks
       }
       for (int i = i0 + tid; i < len; i += NT) count(i, h[i]);
     }
-    if (a.n_bias) sum_biases<NT>(a, b, c0, bias_id, bias_value, s_bias, s_id, s_val, s_base);
+    if (a.n_bias) sum_biases<NT, kPer>(a, b, c0, bias_id, bias_value, s_bias, s_id, s_val, s_base);
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < kPer / 4; ++q) {
@@ -259,10 +263,16 @@ __global__ __launch_bounds__(kLseThreads) void edit_lse_kernel(EditArgs a, int n
   if (r >= (long)a.B * a.K) return;
   const float2* P = a.partials + (size_t)r * nP;
   float mx = -FLT_MAX, sm = 0.f;
-  for (int t = lane; t < nP; t += kWave) {
-    const float2 p = P[t];
-    const float m = fmaxf(mx, p.x);
-    sm = sm * exp_diff(mx, m) + p.y * exp_diff(p.x, m);
+  for (int t0 = lane; t0 < nP; t0 += 8 * kWave) {  // eight loads in flight
+    float2 p[8];
+    float m = mx;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = t0 + j * kWave < nP ? P[t0 + j * kWave] : make_float2(-FLT_MAX, 0.f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = fmaxf(m, p[j].x);
+    sm *= exp_diff(mx, m);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sm += p[j].y * exp_diff(p[j].x, m);
     mx = m;
   }
   const float m = wave_max(mx);
@@ -272,10 +282,10 @@ __global__ __launch_bounds__(kLseThreads) void edit_lse_kernel(EditArgs a, int n
 
 }  // namespace
 
-// A pair per wavefront and chunk, that is per 512 tokens; room for the longest chunk.
-int edit_partials(int V) { return (V + 4095) / 4096 * 8; }
+// A pair per wavefront and chunk: per 256 tokens at most, chunks of up to 4096.
+int edit_partials(int V) { return (V + 4095) / 4096 * 16; }
 
-template <int NT>
+template <int NT, int kPer>
 static void launch_edit_of(const EditArgs& a) {
   const int chunks = (a.V + NT * kPer - 1) / (NT * kPer);
   const long units = (long)chunks * a.B;
@@ -290,8 +300,8 @@ static void launch_edit_of(const EditArgs& a) {
   const long per = most / ((long)chunks * groups);
   for (long b0 = 0; b0 < a.B; b0 += per) {
     const dim3 grid((unsigned)((a.B - b0 < per ? a.B - b0 : per) * chunks * groups));
-    if (a.bf16) hipLaunchKernelGGL((edit_kernel<NT, true>), grid, dim3(NT), 0, a.stream, a, (int)b0, chunks, slots, groups);
-    else hipLaunchKernelGGL((edit_kernel<NT, false>), grid, dim3(NT), 0, a.stream, a, (int)b0, chunks, slots, groups);
+    if (a.bf16) hipLaunchKernelGGL((edit_kernel<NT, kPer, true>), grid, dim3(NT), 0, a.stream, a, (int)b0, chunks, slots, groups);
+    else hipLaunchKernelGGL((edit_kernel<NT, kPer, false>), grid, dim3(NT), 0, a.stream, a, (int)b0, chunks, slots, groups);
   }
   if (a.out_lse) {
     const long rows = (long)a.B * a.K;
@@ -300,10 +310,14 @@ static void launch_edit_of(const EditArgs& a) {
   }
 }
 
-// Chunks of 4096 tokens halve what is read of the histories; below, chunks of 2048 start earlier and fill the CUs more evenly.
+// Threads and tokens per thread.  Many threads per token where a long history has to be counted for every chunk (8 sequences of 65536, 4
+// slots of V = 126464: 23 us, with 512 x 8 28, with 256 x 8 32; of 8192 20 in all three); of large calls 512 x 8 rather than 256 x 8 (32 x 16
+// slots of V = 126464, histories of 8192: 131 against 142); else 256 x 8, which start earlier and fill the CUs more evenly (64 x 4 slots of
+// V = 32000 24 us, with 512 x 8 30).
 hipError_t launch_edit(const EditArgs& a) {
-  if (a.history_max >= 16384 || (long)a.B * a.K * a.V >= 1L << 25) launch_edit_of<512>(a);
-  else launch_edit_of<256>(a);
+  if (a.history_max >= 16384) launch_edit_of<512, 4>(a);
+  else if ((long)a.B * a.K * a.V >= 1L << 25) launch_edit_of<512, 8>(a);
+  else launch_edit_of<256, 8>(a);
   return hipGetLastError();
 }
 
