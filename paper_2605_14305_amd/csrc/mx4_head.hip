@@ -10,6 +10,9 @@
 // Layout.  The multiply adds over k in any order as long as both operands agree on it.  Lane l = (token or row l % 16, group g = l / 16)
 // takes the 32 codes of block 4 u + g (16 bytes and one scale), which feed four multiplies of 8 codes per lane; of h it takes the same
 // columns.  Tokens are the rows of D, so a lane ends with four consecutive tokens of one row of h.
+#include <limits.h>
+
+#include <algorithm>
 #include <type_traits>
 
 #include "head_common.hpp"
@@ -72,7 +75,7 @@ typedef float floatx4_any __attribute__((ext_vector_type(4), aligned(4)));
 // LDS holds a stage's rows one behind another, their 16-byte chunks exchanged within 256 bytes (chunk ^ row, as far as the row length allows) so that
 // 16 rows meet all banks.
 template <int UPW, int MT, bool F32>
-__global__ __launch_bounds__(kThreads, 2) void mx4_stages_kernel(Mx4Args a, int KS) {
+__global__ __launch_bounds__(kThreads, 2) void mx4_stages_kernel(Mx4Args a, int KS, int runs, int row_blocks) {
   constexpr int P = F32 ? 3 : 1, ROWS = 16 * MT;
   constexpr int RING = 3;
   constexpr int kCodes = UPW * kThreads;                       // chunks of 16 bytes per stage
@@ -88,9 +91,12 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_stages_kernel(Mx4Args a, int 
   const int u0 = slice * nu / KS, count = (slice + 1) * nu / KS - u0;  // UPW or UPW - 1
   const int swap = min(nb & -nb, 16) - 1;
   const int tiles = (a.V + 15) / 16;
-  const int run0 = (int)((long)blockIdx.x * tiles / gridDim.x), run1 = (int)((long)(blockIdx.x + 1) * tiles / gridDim.x);
+  // Row blocks of a run go to one XCD one behind another: its codes come from memory once.
+  const int q8 = blockIdx.x >> 3, by = q8 % row_blocks, bx = q8 / row_blocks * 8 + (blockIdx.x & 7);
+  if (bx >= runs) return;
+  const int run0 = (int)((long)bx * tiles / runs), run1 = (int)((long)(bx + 1) * tiles / runs);
   const int stages = (run1 - run0 + TG - 1) / TG;
-  const int row0 = blockIdx.y * ROWS;
+  const int row0 = by * ROWS;
 
   // Where this lane's chunks and its word of scales come from, relative to the stage's first token; `last`: the last token there is.
   auto chunk_at = [&](int i, int last) {
@@ -253,23 +259,33 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_stages_kernel(Mx4Args a, int 
 // Few slices mean few barriers and few partial sums, but every tile of a stage brings its copy of h into registers before the first
 // multiply: one slice wherever h fits (8 rows of d = 512, V = 126464: 11.1 us, in two slices 13.1, in four 16.0), and of more
 // slices the fewest that leave a workgroup eight stages (8 rows of d = 2048, V = 50257 in four slices, six stages: 15.9, in eight 14.7;
-// 16 float32 rows, whose h is three times as long, of d = 1024, V = 32000 in two slices, two stages: 18.1, in eight 11.7).
+// 16 float32 rows, whose h is three times as long, of d = 1024, V = 32000 in two slices, two stages: 18.1, in eight 11.7), but none that
+// gets no column (8 rows of d = 256, V = 32000 in two slices 5.8, in eight, six of them empty, 8.7).
 template <int MT, bool F32>
 bool launch_stages(const Mx4Args& a) {
   const int tiles = (a.V + 15) / 16, nu = (a.d + 127) / 128;
-  if (nu > 4 * kWaves || a.d % 64 || a.d < 128) return false;
+  if (nu > 4 * kWaves || a.d % 64 || a.d < 128 || a.R > 1 << 20) return false;  // a launch holds fewer than 2^32 threads
+  // Rounds of a workgroup per CU, 32 per XCD: more of them leave fewer CUs without work where row blocks do not divide 32; the start of a
+  // run (h, the first stages) costs about 16 tiles.  272 float32 rows of d = 4096, V = 50257, 17 row blocks: 346 us, in one round 523.
+  const int row_blocks = (a.R + 16 * MT - 1) / (16 * MT), first = (row_blocks + 31) / 32;
+  int runs = 0;
+  long least = LONG_MAX;
+  for (int r = first; r < first + 8; ++r) {
+    const int n = std::min(tiles, 32 * r / row_blocks * 8);
+    const long cost = r * ((tiles + n - 1) / n + 16L);
+    if (cost < least) least = cost, runs = n;
+  }
   int KS = 1;
-  while (nu > 4 * KS || (KS < kWaves && tiles < (KS == 1 && !F32 ? 1 : 8) * 256 * (kWaves / KS))) KS *= 2;
-  const dim3 grid(tiles < 256 ? tiles : 256, (a.R + 16 * MT - 1) / (16 * MT));
+  while (nu > 4 * KS || (KS < kWaves && KS < nu && tiles < (KS == 1 && !F32 ? 1 : 8) * runs * (kWaves / KS))) KS *= 2;
+  const dim3 grid((runs + 7) / 8 * 8 * row_blocks);
   switch ((nu + KS - 1) / KS) {
-    case 1: FEF_LAUNCH_HEAD((mx4_stages_kernel<1, MT, F32>), grid, dim3(kThreads), a, a, KS); break;
-    case 2: FEF_LAUNCH_HEAD((mx4_stages_kernel<2, MT, F32>), grid, dim3(kThreads), a, a, KS); break;
-    case 3: FEF_LAUNCH_HEAD((mx4_stages_kernel<3, MT, F32>), grid, dim3(kThreads), a, a, KS); break;
-    default: FEF_LAUNCH_HEAD((mx4_stages_kernel<4, MT, F32>), grid, dim3(kThreads), a, a, KS); break;
+    case 1: FEF_LAUNCH_HEAD((mx4_stages_kernel<1, MT, F32>), grid, dim3(kThreads), a, a, KS, runs, row_blocks); break;
+    case 2: FEF_LAUNCH_HEAD((mx4_stages_kernel<2, MT, F32>), grid, dim3(kThreads), a, a, KS, runs, row_blocks); break;
+    case 3: FEF_LAUNCH_HEAD((mx4_stages_kernel<3, MT, F32>), grid, dim3(kThreads), a, a, KS, runs, row_blocks); break;
+    default: FEF_LAUNCH_HEAD((mx4_stages_kernel<4, MT, F32>), grid, dim3(kThreads), a, a, KS, runs, row_blocks); break;
   }
   return true;
 }
-
 
 __device__ __forceinline__ void request_2(const void* base, uint32_t offset, uint32_t lds_off) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_ushort %0, %1" :: "v"(offset), "s"(base), "s"(lds_off) : "memory");
@@ -563,15 +579,23 @@ __global__ __launch_bounds__(256) void mx4_kernel(Mx4Args a) {
 
 }  // namespace
 
+// float32 rows go through stages, 16 at a time: there h is split once per workgroup, in tiles before every use (us, stages and tiles; d =
+// 4096, V = 50257: 96 rows 118, 251, 512 rows 527, 869; 32 rows of V = 126464 112, 163), unless the head is small and the runs so short that
+// starting them tells (64 rows of d = 256, V = 50257 19.6, 15.0; 32 of d = 768, V = 50257 22.2, 18.9; 40 of d = 896, V = 20000 16.2, 26.1).
+// bf16 rows go through stages up to 32; above them only where the vocabulary makes too few tiles for all CUs, so that slices of k
+// are needed (64 rows of d = 4096, V = 8000 17.7, 26; 300 of d = 2048, V = 1000 10.4, 18.2; but 64 of V = 126464 105, 94; 512 of d = 1024, V =
+// 8000 27.7, 13.7).
 hipError_t launch_mx4(const Mx4Args& a) {
+  const long rv = (long)a.R * a.V;
   if (a.d % 64 == 0) {
     if (a.f32) {
-      if (a.R <= 16 && launch_stages<1, true>(a)) return hipGetLastError();
+      const bool tiles = a.R > 16 && a.d < 896 && a.V >= 16384 && rv < 1L << 22;
+      if (!tiles && launch_stages<1, true>(a)) return hipGetLastError();
       if (a.R <= 32) launch_tile<1, 2, true>(a);
       else launch_tile<2, 2, true>(a);
     } else {
       if (a.R <= 16 && launch_stages<1, false>(a)) return hipGetLastError();
-      if (a.R <= 32 && launch_stages<2, false>(a)) return hipGetLastError();
+      if ((a.R <= 32 || (a.V <= 8192 && rv <= 1L << 20)) && launch_stages<2, false>(a)) return hipGetLastError();
       const int blocks = (a.R + 127) / 128, rows = (a.R + blocks - 1) / blocks;
       if (rows <= 32) launch_tile<2, 1, false>(a);
       else if (rows <= 48) launch_tile<3, 1, false>(a);

@@ -60,6 +60,45 @@ def test_sizes(R, d, V, dtype):
     _check(out, h, _dense(codes, scales), float(np.float32(tau)), dtype)
 
 
+# vocabularies and hidden sizes from which on many rows go through tiles; many row blocks through stages
+LONG = [(33, 192, 8200), (48, 320, 9001), (64, 256, 8195), (65, 448, 8200), (96, 192, 8333), (100, 128, 8200), (130, 64, 8201), (150, 576, 8207),
+        (300, 256, 4001), (17, 192, 16400), (50, 320, 16385), (40, 704, 20001), (40, 4160, 200), (20, 4224, 150), (130, 4352, 97),
+        (272, 1024, 333), (528, 128, 2000), (100, 2112, 70), (600, 192, 50)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,d,V", LONG)
+def test_sizes_with_many_rows(R, d, V, dtype):
+    rng = np.random.default_rng(R * 7919 + d * 31 + V)
+    codes, scales = _weights(rng, V, d)
+    h = _hidden(rng, R, d, dtype)
+    tau = (1.0, 0.7, 3.0)[V % 3]
+    out = fb.Mx4Logits(R, d, V, dtype)(h.cuda(), torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), temperature=tau)
+    _check(out, h, _dense(codes, scales), float(np.float32(tau)), dtype)
+
+
+@pytest.mark.parametrize("dtype,R,V", [("bf16", 40, 8300), ("bf16", 100, 8300), ("bf16", 300, 8301), ("f32", 20, 16400), ("f32", 50, 16401)])
+def test_infinities_and_nan_in_tiles(dtype, R, V):
+    rng = np.random.default_rng(R)
+    d = 192
+    codes, scales = _weights(rng, V, d, 120, 130)
+    codes |= 0x11
+    scales[7, 3] = scales[V - 1, 5] = 255
+    h = _hidden(rng, R, d, dtype)
+    h[0, 5], h[1, 100] = float("inf"), float("nan")
+    whole = torch.full((R + 2, V + 13), -7.0, device="cuda")
+    fb.Mx4Logits(R, d, V, dtype)(h.cuda(), torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), out=whole[1:R + 1, 5:5 + V])
+    out = whole[1:R + 1, 5:5 + V].cpu()
+    good = torch.ones(V, dtype=torch.bool)
+    good[[7, V - 1]] = False
+    w = _dense(codes, scales)[good.numpy()]
+    assert bool(torch.isnan(out[:, ~good]).all()) and bool(torch.isnan(out[1]).all())
+    assert bool((out[0, good].double() == torch.from_numpy(np.sign(w[:, 5])) * float("inf")).all())
+    _check(out[2:, good], h[2:], w, 1.0, dtype)
+    whole[1:R + 1, 5:5 + V] = -7.0
+    assert bool((whole == -7.0).all())
+
+
 @pytest.mark.parametrize("R,V", [(1, 100), (5, 333), (40, 70), (300, 97)])
 def test_output_rows_further_apart_and_nothing_else_written(R, V):
     rng = np.random.default_rng(R)
