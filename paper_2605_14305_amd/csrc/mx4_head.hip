@@ -321,7 +321,11 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_tile_kernel(Mx4Args a, int ru
   constexpr int NI = HI > CI ? HI : CI;
   uint32_t off[NI], s_off[SI];
   auto piece_of = [&](int i) { return (i * 4 + quarter) * kWave + lane; };
-  auto h_column = [&](int i) { const int s = piece_of(i); return (s & (8 * kElem - 1)) ^ (s / (8 * kElem) & 15); };
+  // Where a row's 16-byte chunks lie: exchanged by fold(row), so that 16 lanes which are served together, eight rows of one group g and
+  // the other eight of the next, meet all banks (rows 0-3 and 12-15, and 4-11 of the next group).  Exchanged by the row itself, every read
+  // took twice its cycles (64 rows of d = 4096, V = 126464: 94.8 us, so 91.1).
+  auto fold = [](int row) { return (row ^ (F32 ? row >> 1 & 4 : row << 1 & 8)) & 15; };
+  auto h_column = [&](int i) { const int s = piece_of(i); return (s & (8 * kElem - 1)) ^ fold(s / (8 * kElem)); };
   auto c_chunk = [&](int i) { const int s = piece_of(i); return (s & 7) ^ (s >> 4 & 7); };
   if (!asks_codes) {
 #pragma unroll
@@ -410,11 +414,11 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_tile_kernel(Mx4Args a, int ru
         if constexpr (F32) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            f[e][m] = reinterpret_cast<const floatx4*>(s_h)[row * 32 + ((8 * g + 2 * j + e) ^ i16)];
+            f[e][m] = reinterpret_cast<const floatx4*>(s_h)[row * 32 + ((8 * g + 2 * j + e) ^ fold(i16))];
             if (half) f[e][m] = __builtin_bit_cast(floatx4, __builtin_bit_cast(intx4, f[e][m]) & keep);
           }
         } else {
-          x[j & 1][0][m] = s_h[row * 16 + ((4 * g + j) ^ i16)];
+          x[j & 1][0][m] = s_h[row * 16 + ((4 * g + j) ^ fold(i16))];
           if (half) x[j & 1][0][m] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(intx4, x[j & 1][0][m]) & keep);
         }
       }
