@@ -525,29 +525,40 @@ __global__ __launch_bounds__(kSumThreads) void row_sums_draft_kernel(VerifyArgs 
 }
 
 // ---------------------------------------------------------------------------------------------
-// In front of kernel 1 where the caller brings the logits: (max, sum exp) of each row's 256-token tiles, a wavefront per tile, four
-// tokens per lane.  Bound: one read of the logits.
+// In front of kernel 1 where the caller brings the logits: (max, sum exp) of each row's 256-token tiles, a wavefront per two tiles, four
+// tokens of each per lane, both loads in flight.  Bound: one read of the logits (1024 rows of V = 151936, 622 MB, in 109 us, 5.7 TB/s; a
+// whole round on them 121 us, with one tile per wavefront 147, with four 127; on 16 rows of V = 126464 16.0, 18.0, 16.3).
 // ---------------------------------------------------------------------------------------------
+constexpr int kPartialTiles = 2;
+
 __global__ __launch_bounds__(NT) void logit_partials_kernel(VerifyArgs a, int row, int groups) {
   constexpr float kLog2e = 1.4426950408889634f;
+  constexpr int T = kPartialTiles;
   const int lane = threadIdx.x & 63;
   const unsigned r = blockIdx.x / (unsigned)groups;
-  const int t = (int)(blockIdx.x - r * (unsigned)groups) * NW + (threadIdx.x >> 6);
-  if (t >= a.nT) return;
-  const int v = t * kTiled256Tn + 4 * lane;
-  floatx4 l = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  if (v < a.V) {  // rows are padded to 64 tokens
-    l = *reinterpret_cast<const floatx4*>(a.logits + (size_t)(row + r) * a.ldl + v);
+  const int t0 = ((int)(blockIdx.x - r * (unsigned)groups) * NW + (threadIdx.x >> 6)) * T;
+  const float* logits = a.logits + (size_t)(row + r) * a.ldl;
+  floatx4 l[T];
+#pragma unroll
+  for (int i = 0; i < T; ++i) {
+    const int v = (t0 + i) * kTiled256Tn + 4 * lane;
+    l[i] = floatx4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (v < a.V) l[i] = *reinterpret_cast<const floatx4*>(logits + v);  // rows are padded to 64 tokens
+  }
+#pragma unroll
+  for (int i = 0; i < T; ++i) {
+    const int t = t0 + i, v = t * kTiled256Tn + 4 * lane;
+    if (t >= a.nT) return;
 #pragma unroll
     for (int j = 1; j < 4; ++j)
-      if (v + j >= a.V) l[j] = -INFINITY;
-  }
-  const float mx = wave_max(fmaxf(fmaxf(fmaxf(fmaxf(l[0], l[1]), l[2]), l[3]), kLowest));
-  float e = 0.f;
+      if (v + j >= a.V) l[i][j] = -INFINITY;
+    const float mx = wave_max(fmaxf(fmaxf(fmaxf(fmaxf(l[i][0], l[i][1]), l[i][2]), l[i][3]), kLowest));
+    float e = 0.f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) e += __builtin_amdgcn_exp2f((l[j] - mx) * kLog2e);
-  e = wave_sum(e);
-  if (lane == 0) const_cast<float2*>(a.partials)[(size_t)(row + r) * a.nT + t] = make_float2(mx, e);
+    for (int j = 0; j < 4; ++j) e += __builtin_amdgcn_exp2f((l[i][j] - mx) * kLog2e);
+    e = wave_sum(e);
+    if (lane == 0) const_cast<float2*>(a.partials)[(size_t)(row + r) * a.nT + t] = make_float2(mx, e);
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1204,7 +1215,7 @@ hipError_t launch_toy_round(const HeadArgs& h, const VerifyArgs& a) {
 }
 
 hipError_t launch_logit_partials(const VerifyArgs& a) {
-  const int groups = (a.nT + NW - 1) / NW;
+  const int groups = (a.nT + NW * kPartialTiles - 1) / (NW * kPartialTiles);
   const long most = ((1L << 32) / NT - 1) / groups;  // rows of a launch of fewer than 2^32 threads
   for (long r0 = 0; r0 < a.nrows; r0 += most) {
     const long rows = a.nrows - r0 < most ? a.nrows - r0 : most;
