@@ -43,8 +43,8 @@ __device__ __forceinline__ float divided(float x, float y, float r) {
   return fabsf(q) < INFINITY ? __builtin_fmaf(e, r, q) : q;
 }
 
-// Biases of the chunk's tokens, summed per token in the order of the list (its first NT entries are given): the entries that name one of them are packed in order, and
-// the first of each token adds up its like.
+// Biases of the chunk's tokens, summed per token in the order of the list (its first NT entries are given): the entries that name one of
+// them are packed in order, and the first of each token adds up its like.
 template <int NT, int kPer>
 __device__ void sum_biases(const EditArgs& a, int b, int c0, int id0, float value0, float* s_bias, int* s_id, float* s_val, int* s_base) {
   constexpr int NW = NT / kWave, kChunk = NT * kPer;

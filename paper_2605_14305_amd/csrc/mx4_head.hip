@@ -67,13 +67,18 @@ __device__ __forceinline__ void request_4(const void* base, uint32_t offset, uin
 
 typedef float floatx4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-// Up to 16 MT rows whose h fits the registers.  A workgroup per CU takes a run of 16-token tiles in stages of TG of them, up to 32 KB of
-// codes and 2 KB of scales, which come in the order of memory straight into LDS, RING - 1 stages ahead.  Its eight wavefronts are KS slices of
-// k times TG = 8 / KS tiles: a wavefront holds its slice of h as operands for the whole kernel (UPW units of 128 columns) and multiplies
-// its codes of each stage with it; the KS partial sums of a tile meet in LDS and are added in the order of the slices by one
-// wavefront, in turn, while the next stage is multiplied.  One barrier per stage.
-// LDS holds a stage's rows one behind another, their 16-byte chunks exchanged within 256 bytes (chunk ^ row, as far as the row length allows) so that
-// 16 rows meet all banks.
+// Rows whose h fits the registers, 16 MT at a time.  A workgroup per CU takes a run of 16-token tiles in stages of TG of them, up to 32 KB
+// of codes and 2 KB of scales, which come in the order of memory straight into LDS, RING - 1 stages ahead.  Its eight wavefronts are KS
+// slices of k times TG = 8 / KS tiles: a wavefront holds its slice of h as operands for the whole kernel (UPW units of 128 columns) and
+// multiplies its codes of each stage with it; the KS partial sums of a tile meet in LDS and are added in the order of the slices by one
+// thread per sum while the next stage is multiplied.  One barrier per stage.
+// LDS holds a stage's rows one behind another, their 16-byte chunks exchanged within 256 bytes (chunk ^ row, as far as the row length
+// allows) so that 16 rows meet all banks.
+// Bound: the read of the codes.  8 rows of d = 4096, V = 126464 (279 MB) 51.6 us, 5.4 TB/s; a plain read of as much takes 45 to 46.  Stages of
+// 32 KB in the order of memory are what carries it: codes loaded from memory into registers by the wavefronts that
+// use them took 70.  With 32 rows 63 to 67 us.  Of a short head the start (launch, h, the first stage's way from memory: 4 of the 5
+// us at d = 512, V = 5000) and a barrier per stage count (16 float32 rows of d = 1024, V = 32000, eight stages of 8 KB: 11.6 us against 3.2
+// of bytes); a ring of five or six such stages changes nothing (12.1, 12.4).
 template <int UPW, int MT, bool F32>
 __global__ __launch_bounds__(kThreads, 2) void mx4_stages_kernel(Mx4Args a, int KS, int runs, int row_blocks) {
   constexpr int P = F32 ? 3 : 1, ROWS = 16 * MT;
@@ -204,11 +209,11 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_stages_kernel(Mx4Args a, int 
     if (ahead == 1) wait_newer<UPW + 1>();
     else wait_newer<0>();
     const int tok0 = (run0 + n * TG) * 16;
-    if (tok0 + TG * 16 > a.V && (((a.V - tok0) * nb) & 3)) {  // an odd vocabulary, rows of 2 + 4 n scales: the last two
-      const int at = (a.V - tok0) * nb - 2;
+    if (tok0 + TG * 16 > a.V && (((a.V - tok0) * nb) & 3)) {  // the vocabulary's last scales are no whole word
+      const int at = (a.V - tok0) * nb & ~3, bytes = (a.V - tok0) * nb & 3;
       if (tid == at / 4) {  // the thread whose request filled this word
         const uint8_t* from = a.scales + (size_t)tok0 * nb + at;
-        s_scales[n % RING][tid] = from[0] | from[1] << 8;
+        s_scales[n % RING][tid] = from[0] | (bytes > 1 ? from[1] << 8 : 0) | (bytes > 2 ? from[2] << 16 : 0);
       }
     }
     lds_barrier();
@@ -264,7 +269,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_stages_kernel(Mx4Args a, int 
 template <int MT, bool F32>
 bool launch_stages(const Mx4Args& a) {
   const int tiles = (a.V + 15) / 16, nu = (a.d + 127) / 128;
-  if (nu > 4 * kWaves || a.d % 64 || a.d < 128 || a.R > 1 << 20) return false;  // a launch holds fewer than 2^32 threads
+  if (nu > 4 * kWaves || a.d < 128 || a.R > 1 << 20) return false;  // a launch holds fewer than 2^32 threads
   // Rounds of a workgroup per CU, 32 per XCD: more of them leave fewer CUs without work where row blocks do not divide 32; the start of a
   // run (h, the first stages) costs about 16 tiles.  272 float32 rows of d = 4096, V = 50257, 17 row blocks: 346 us, in one round 523.
   const int row_blocks = (a.R + 16 * MT - 1) / (16 * MT), first = (row_blocks + 31) / 32;
@@ -291,11 +296,15 @@ __device__ __forceinline__ void request_2(const void* base, uint32_t offset, uin
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_ushort %0, %1" :: "v"(offset), "s"(base), "s"(lds_off) : "memory");
 }
 
-// More rows: a workgroup takes a run of up to WC TT tiles times 16 M WR rows through steps of 128 columns.  Its eight wavefronts are WR groups of
-// 16 M rows times WC = 8 / WR columns of tiles, wavefront column c with the tiles c, c + WC, ... of the run: codes become bf16 where they are used,
-// once for 16 M rows, and a fragment of h serves TT tiles.  All of it is requested straight into LDS: h, which L2 holds, one step ahead by
-// wavefronts 0 to 3, and whole 128-byte lines of codes, two steps at a time, up to four steps ahead by the others (requests of one
-// wavefront complete in order, so one that had asked for both would wait for the far ones with the near ones).
+// More rows: a workgroup takes a run of up to WC TT tiles times 16 M WR rows through steps of 128 columns.  Its eight wavefronts are WR
+// groups of 16 M rows times WC = 8 / WR columns of tiles, wavefront column c with the tiles c, c + WC, ... of the run: codes become bf16
+// where they are used, once for 16 M rows, and a fragment of h serves TT tiles.  All of it is requested straight into LDS: h, which L2
+// holds, one step ahead by wavefronts 0 to 3, and whole 128-byte lines of codes, two steps at a time, up to four steps ahead by the others
+// (requests of one wavefront complete in order, so one that had asked for both would wait for the far ones with the near ones).
+// Bound: the multiplies.  512 rows of d = 3584, V = 151936: 488 to 504 us, 1.11 to 1.14 PFLOP/s, a plain bf16 product of 8192^3 1.22; the
+// transfers alone take 313, the multiplies alone 382.  With fewer rows neither covers the other well, since the wavefronts meet at
+// a barrier per step: 64 rows of d = 4096, V = 126464 91 us, transfers alone 75 (59 without h), multiplies alone 63, bytes 51.  h two
+// steps ahead (93 to 95) or four tiles of tokens per wavefront with a single step of h in LDS (96) are no better.
 template <int M, int WR, int TT, bool F32>
 __global__ __launch_bounds__(kThreads, 2) void mx4_tile_kernel(Mx4Args a, int runs, int row_blocks) {
   constexpr int P = F32 ? 3 : 1, WC = 8 / WR, ROWS = 16 * M * WR, TOK = 16 * WC * TT, kElem = F32 ? 4 : 2;
@@ -522,7 +531,9 @@ void launch_tile(const Mx4Args& a) {
 
 constexpr int kRowsPerWave = 64;
 
-// Rows of d = 32 (2 n + 1), which are no whole pairs of blocks: a wavefront per 16 tokens and 64 rows, straight from memory; grid (groups of 64 tokens, groups of 64 rows).
+// Rows of d = 32 (2 n + 1) below 128 or above 4096: a wavefront per 16 tokens and 64 rows, straight from memory; grid (groups of 64 tokens,
+// groups of 64 rows).  Bound: the latency of its loads, a step of 128 columns after another: 8 rows of d = 4128, V = 126464
+// 352 us (of d = 4160 in tiles 84).  Sizes of models are not among them.
 template <bool F32>
 __global__ __launch_bounds__(256) void mx4_kernel(Mx4Args a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -586,26 +597,34 @@ __global__ __launch_bounds__(256) void mx4_kernel(Mx4Args a) {
 // float32 rows go through stages, 16 at a time: there h is split once per workgroup, in tiles before every use (us, stages and tiles; d =
 // 4096, V = 50257: 96 rows 118, 251, 512 rows 527, 869; 32 rows of V = 126464 112, 163), unless the head is small and the runs so short that
 // starting them tells (64 rows of d = 256, V = 50257 19.6, 15.0; 32 of d = 768, V = 50257 22.2, 18.9; 40 of d = 896, V = 20000 16.2, 26.1).
-// bf16 rows go through stages up to 32; above them only where the vocabulary makes too few tiles for all CUs, so that slices of k
-// are needed (64 rows of d = 4096, V = 8000 17.7, 26; 300 of d = 2048, V = 1000 10.4, 18.2; but 64 of V = 126464 105, 94; 512 of d = 1024, V =
-// 8000 27.7, 13.7).
+// bf16 rows go through stages up to 32; above them only where the vocabulary makes too few tiles for all CUs, so that slices of k are
+// needed (64 rows of d = 4096, V = 8000 17.7, 26; 300 of d = 2048, V = 1000 10.4, 18.2; but 64 of V = 126464 105, 94; 512 of d = 1024,
+// V = 8000 27.7, 13.7), and where d is no whole number of 64, which tiles do not do (64 rows of d = 1056, V = 50257 25.2; of 1024 14.5).
 hipError_t launch_mx4(const Mx4Args& a) {
   const long rv = (long)a.R * a.V;
-  if (a.d % 64 == 0) {
+  const bool lines = a.d % 64 == 0;  // whole pairs of blocks, which tiles need
+  if (a.f32) {
+    const bool tiles = lines && a.R > 16 && a.d < 896 && a.V >= 16384 && rv < 1L << 22;
+    if (!tiles && launch_stages<1, true>(a)) return hipGetLastError();
+  } else {
+    if (a.R <= 16 && launch_stages<1, false>(a)) return hipGetLastError();
+    if ((a.R <= 32 || !lines || (a.V <= 8192 && rv <= 1L << 20)) && launch_stages<2, false>(a)) return hipGetLastError();
+  }
+  if (lines) {
+    const int blocks = (a.R + 127) / 128, rows = (a.R + blocks - 1) / blocks;
     if (a.f32) {
-      const bool tiles = a.R > 16 && a.d < 896 && a.V >= 16384 && rv < 1L << 22;
-      if (!tiles && launch_stages<1, true>(a)) return hipGetLastError();
       if (a.R <= 32) launch_tile<1, 2, true>(a);
       else launch_tile<2, 2, true>(a);
+    } else if (rows <= 32) {
+      launch_tile<2, 1, false>(a);
+    } else if (rows <= 48) {
+      launch_tile<3, 1, false>(a);
+    } else if (rows <= 64) {
+      launch_tile<4, 1, false>(a);
+    } else if (rows <= 96) {
+      launch_tile<3, 2, false>(a);
     } else {
-      if (a.R <= 16 && launch_stages<1, false>(a)) return hipGetLastError();
-      if ((a.R <= 32 || (a.V <= 8192 && rv <= 1L << 20)) && launch_stages<2, false>(a)) return hipGetLastError();
-      const int blocks = (a.R + 127) / 128, rows = (a.R + blocks - 1) / blocks;
-      if (rows <= 32) launch_tile<2, 1, false>(a);
-      else if (rows <= 48) launch_tile<3, 1, false>(a);
-      else if (rows <= 64) launch_tile<4, 1, false>(a);
-      else if (rows <= 96) launch_tile<3, 2, false>(a);
-      else launch_tile<4, 2, false>(a);
+      launch_tile<4, 2, false>(a);
     }
     return hipGetLastError();
   }

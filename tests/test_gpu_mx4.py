@@ -63,7 +63,9 @@ def test_sizes(R, d, V, dtype):
 # vocabularies and hidden sizes from which on many rows go through tiles; many row blocks through stages
 LONG = [(33, 192, 8200), (48, 320, 9001), (64, 256, 8195), (65, 448, 8200), (96, 192, 8333), (100, 128, 8200), (130, 64, 8201), (150, 576, 8207),
         (300, 256, 4001), (17, 192, 16400), (50, 320, 16385), (40, 704, 20001), (40, 4160, 200), (20, 4224, 150), (130, 4352, 97),
-        (272, 1024, 333), (528, 128, 2000), (100, 2112, 70), (600, 192, 50)]
+        (272, 1024, 333), (528, 128, 2000), (100, 2112, 70), (600, 192, 50),
+        # odd numbers of blocks, with every remainder of the vocabulary by four
+        (1, 160, 1000), (8, 2080, 1001), (16, 1056, 20002), (17, 3616, 303), (40, 160, 8195), (70, 4064, 97), (300, 992, 150), (5, 96, 9001), (40, 4128, 70)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
