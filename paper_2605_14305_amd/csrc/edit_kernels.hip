@@ -6,7 +6,7 @@
 //                    so nothing waits: slot m + 1 differs from slot m by one token of the prefix, which that token's owner adds.  Per slot
 //                    the logits are read once, written once, and leave a (max, sum exp) pair per wavefront.  A bit per token says
 //                    whether it has an entry; the others see a multiplication and the mask.
-//   edit_lse_kernel  a wavefront per row merges the pairs.
+//   edit_lse_kernel  a wavefront per row merges the pairs, where a row is more than one chunk.
 //
 // Counts are whole numbers, and a token's biases are added in the order of their list, so nothing depends on the order in which
 // threads arrive.
@@ -85,8 +85,8 @@ __device__ void sum_biases(const EditArgs& a, int b, int c0, int id0, float valu
   }
 }
 
-// Workgroup: (sequence, chunk, group of `slots` slots), slots innermost; sequences from b0 on.
-template <int NT, int kPer, bool BF16>
+// Workgroup: (sequence, chunk, group of `slots` slots), slots innermost; sequences from b0 on.  WHOLE: the chunk is the vocabulary.
+template <int NT, int kPer, bool BF16, bool WHOLE>
 __global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks, int slots, int groups) {
   constexpr int NW = NT / kWave, kChunk = NT * kPer;
   __shared__ __attribute__((aligned(16))) unsigned s_cnt[kChunk];
@@ -94,6 +94,7 @@ __global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks
   __shared__ int s_id[NT];
   __shared__ float s_val[NT];
   __shared__ int s_base[NW];
+  __shared__ float2 s_pair[WHOLE ? 2 : 1][NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const unsigned per_chunk = blockIdx.x / (unsigned)groups;
   const int m0 = (int)(blockIdx.x - per_chunk * (unsigned)groups) * slots, m1 = min(m0 + slots, a.K);
@@ -249,7 +250,17 @@ __global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks
 #pragma unroll
     for (int i = 0; i < kPer; ++i) sum += exp_diff(y[i], mx);
     sum = wave_sum(sum);
-    if (lane == 0) a.partials[((size_t)b * a.K + m) * (size_t)(chunks * NW) + chunk * NW + wave] = make_float2(mx, sum);
+    if constexpr (!WHOLE) {
+      if (lane == 0) a.partials[((size_t)b * a.K + m) * (size_t)(chunks * NW) + chunk * NW + wave] = make_float2(mx, sum);
+    } else if (a.out_lse) {  // the row's pairs are all here
+      if (lane == 0) s_pair[m & 1][wave] = make_float2(mx, sum);
+      __syncthreads();
+      if (wave == 0) {
+        const float2 pair = lane < NW ? s_pair[m & 1][lane] : make_float2(-FLT_MAX, 0.f);
+        const float top = wave_max(pair.x), all = wave_sum(pair.y * exp_diff(pair.x, top));
+        if (lane == 0) a.out_lse[(size_t)b * a.K + m] = top + logf(all);
+      }
+    }
     if (prefix) add_prefix(m);
   }
 }
@@ -285,7 +296,7 @@ __global__ __launch_bounds__(kLseThreads) void edit_lse_kernel(EditArgs a, int n
 // A pair per wavefront and chunk: per 256 tokens at most, chunks of up to 4096.
 int edit_partials(int V) { return (V + 4095) / 4096 * 16; }
 
-template <int NT, int kPer>
+template <int NT, int kPer, bool WHOLE = false>
 static void launch_edit_of(const EditArgs& a) {
   const int chunks = (a.V + NT * kPer - 1) / (NT * kPer);
   const long units = (long)chunks * a.B;
@@ -300,10 +311,10 @@ static void launch_edit_of(const EditArgs& a) {
   const long per = most / ((long)chunks * groups);
   for (long b0 = 0; b0 < a.B; b0 += per) {
     const dim3 grid((unsigned)((a.B - b0 < per ? a.B - b0 : per) * chunks * groups));
-    if (a.bf16) hipLaunchKernelGGL((edit_kernel<NT, kPer, true>), grid, dim3(NT), 0, a.stream, a, (int)b0, chunks, slots, groups);
-    else hipLaunchKernelGGL((edit_kernel<NT, kPer, false>), grid, dim3(NT), 0, a.stream, a, (int)b0, chunks, slots, groups);
+    if (a.bf16) hipLaunchKernelGGL((edit_kernel<NT, kPer, true, WHOLE>), grid, dim3(NT), 0, a.stream, a, (int)b0, chunks, slots, groups);
+    else hipLaunchKernelGGL((edit_kernel<NT, kPer, false, WHOLE>), grid, dim3(NT), 0, a.stream, a, (int)b0, chunks, slots, groups);
   }
-  if (a.out_lse) {
+  if (a.out_lse && !WHOLE) {
     const long rows = (long)a.B * a.K;
     constexpr int kRows = kLseThreads / kWave;
     hipLaunchKernelGGL(edit_lse_kernel, dim3((unsigned)((rows + kRows - 1) / kRows)), dim3(kLseThreads), 0, a.stream, a, chunks * (NT / kWave));
@@ -313,10 +324,13 @@ static void launch_edit_of(const EditArgs& a) {
 // Threads and tokens per thread.  Many threads per token where a long history has to be counted for every chunk (8 sequences of 65536, 4
 // slots of V = 126464: 23 us, with 512 x 8 28, with 256 x 8 32; of 8192 20 in all three); of large calls 512 x 8 rather than 256 x 8 (32 x 16
 // slots of V = 126464, histories of 8192: 131 against 142); else 256 x 8, which start earlier and fill the CUs more evenly (64 x 4 slots of
-// V = 32000 24 us, with 512 x 8 30).
+// V = 32000 24 us, with 512 x 8 30).  Where such a chunk holds the vocabulary it also finishes the row, without a second launch (one row of
+// V = 2000 9.2 -> 7.9 us, 64 x 8 slots of it 12.6 -> 10.4; larger workgroups that hold 8000 tokens lose more by waiting for each
+// other in every slot: 64 x 16 slots 25 -> 45).
 hipError_t launch_edit(const EditArgs& a) {
   if (a.history_max >= 16384) launch_edit_of<512, 4>(a);
   else if ((long)a.B * a.K * a.V >= 1L << 25) launch_edit_of<512, 8>(a);
+  else if (a.V <= 2048) launch_edit_of<256, 8, true>(a);
   else launch_edit_of<256, 8>(a);
   return hipGetLastError();
 }
