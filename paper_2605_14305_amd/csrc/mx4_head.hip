@@ -301,7 +301,7 @@ __device__ __forceinline__ void request_2(const void* base, uint32_t offset, uin
 // where they are used, once for 16 M rows, and a fragment of h serves TT tiles.  All of it is requested straight into LDS: h, which L2
 // holds, one step ahead by wavefronts 0 to 3, and whole 128-byte lines of codes, two steps at a time, up to four steps ahead by the others
 // (requests of one wavefront complete in order, so one that had asked for both would wait for the far ones with the near ones).
-// Bound: the multiplies.  512 rows of d = 3584, V = 151936: 488 to 504 us, 1.11 to 1.14 PFLOP/s, a plain bf16 product of 8192^3 1.22; the
+// Bound: the multiplies.  512 rows of d = 3584, V = 151936: 488 to 515 us, 1.08 to 1.14 PFLOP/s, a plain bf16 product of 8192^3 1.22; the
 // transfers alone take 313, the multiplies alone 382.  With fewer rows neither covers the other well, since the wavefronts meet at
 // a barrier per step: 64 rows of d = 4096, V = 126464 91 us, transfers alone 75 (59 without h), multiplies alone 63, bytes 51.  h two
 // steps ahead (93 to 95) or four tiles of tokens per wavefront with a single step of h in LDS (96) are no better.
