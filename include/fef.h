@@ -271,7 +271,7 @@ fef_status fef_head_cross_entropy(const fef_params* prm, const void* h, const vo
  *   out_logits [R, ld]     device float, 4-byte aligned, ld >= V; columns from V on are not touched
  * w and bf16 hidden states are exact in the multiply, float32 ones too (taken as three bf16 parts; what lies below 2^-133 is lost);
  * sums are held in 32 bits, in an order that the sizes decide.
- * Fields of prm that are read: struct_size, d (a positive multiple of 32, at most 2^20), V, dtype, temperature, stream, ev_head_begin /
+ * Fields of prm that are read: struct_size, d (a positive multiple of 32, at most 2^20), V (at most 2^29), dtype, temperature, stream, ev_head_begin /
  * ev_head_end (around the kernel).  1 <= R <= 2^24.  No workspace.  Same conventions and error behaviour as fef_verify_step. */
 fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* codes, const uint8_t* scales, int32_t R,
                           float* out_logits, int64_t ld);
@@ -287,14 +287,14 @@ fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* c
  * computed in float32.  Ids outside [0, V) in any list (-1 pads a list) stand for no token. */
 typedef struct {
   uint32_t struct_size;        /* = sizeof(fef_edit_params)                                        */
-  int32_t B, K, V;             /* sequences, window slots (<= FEF_MAX_K), vocabulary               */
+  int32_t B, K, V;             /* sequences, window slots (<= FEF_MAX_K), vocabulary (<= 2^29)     */
   int32_t dtype;               /* fef_dtype of the logits                                          */
   float temperature;           /* tau > 0                                                          */
   int64_t seq_stride;          /* elements from a sequence's logits to the next one's, >= 0        */
   int64_t slot_stride;         /* elements from a slot's logits to the next one's, >= 0            */
   int64_t out_seq_stride;      /* the same of the output; rows of the output must not overlap      */
   int64_t out_slot_stride;
-  int32_t history_max;         /* columns of history; 0: no history                                */
+  int32_t history_max;         /* columns of history, at most 2^30; 0: no history                  */
   const int32_t* history;      /* [B, history_max], NULL with history_max == 0                     */
   const int32_t* history_len;  /* [B] tokens in use, clamped to [0, history_max]; NULL: all        */
   const int32_t* prompt_len;   /* [B] of these the prompt, clamped to history_len; NULL: none      */
@@ -302,7 +302,7 @@ typedef struct {
   const float* repetition;     /* [B] each, NULL: 1, 0 and 0                                       */
   const float* presence;
   const float* frequency;
-  int32_t n_bias;              /* entries of a bias list; 0: no biases                             */
+  int32_t n_bias;              /* entries of a bias list, at most 2^30; 0: no biases               */
   const int32_t* bias_ids;     /* [B, n_bias]                                                      */
   const float* bias_values;    /* [B, n_bias]                                                      */
   int32_t masks;               /* 0: no masks, 1: one per sequence, K: one per slot                */
@@ -330,7 +330,7 @@ fef_status fef_edit_logits(const fef_edit_params* prm, const void* logits, float
  *           divided by the temperature.  -inf marks a token that a law does not have; columns from V on are read but ignored.  A row
  *           of nothing but -inf is no law: a slot with such a row is rejected (the greedy variant takes the row for token 0), and
  *           its token, in [0, V) and with a confidence that may be NaN, means nothing
- * Fields of prm that are read: as in fef_verify_step but for d, dtype, temperature, gemm_variant; ev_head_begin and ev_head_end
+ * Fields of prm that are read: as in fef_verify_step but for d, dtype, temperature, gemm_variant; V is at most 2^29, ev_head_begin and ev_head_end
  * must be NULL.  Workspace: fef_verify_logits_workspace_bytes (0 if the arguments are invalid). */
 size_t fef_verify_logits_workspace_bytes(const fef_params* prm, int32_t K, int32_t block);
 fef_status fef_verify_logits(const fef_params* prm, const float* logits, int64_t ld, int32_t K, int32_t block, uint64_t seed,

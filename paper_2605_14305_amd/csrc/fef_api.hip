@@ -535,11 +535,16 @@ fef_status fef_head_cross_entropy(const fef_params* prm, const void* h, const vo
 }
 
 namespace {
+// Largest vocabulary of the calls below and longest list of an edit: token and list indices of the kernels, rounded up to whole tiles and
+// one step further, then stay in 32 bits with their sign, and a grid of 16-token tiles below 2^32 threads.
+constexpr int kMaxGivenV = 1 << 29, kMaxList = 1 << 30;
+
 // A call on given logits as one of a 256-token head: a partial per tile, whatever made the logits.
 fef_status logits_params(const fef_params* prm, fef_params* p) {
   if (!prm) return fail(FEF_ERR_INVALID_ARG, "params is NULL");
   if (prm->struct_size != sizeof(fef_params))
     return fail(FEF_ERR_INVALID_ARG, "struct_size %u does not match this library's %zu", prm->struct_size, sizeof(fef_params));
+  if (prm->V > kMaxGivenV) return fail(FEF_ERR_INVALID_ARG, "V = %d exceeds 2^29", prm->V);
   *p = *prm;
   p->d = 64; p->dtype = FEF_BF16; p->gemm_variant = FEF_GEMM_TILED256; p->temperature = 1.f;
   return FEF_OK;
@@ -573,6 +578,7 @@ fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* c
     return fail(FEF_ERR_INVALID_ARG, "struct_size %u does not match this library's %zu", prm->struct_size, sizeof(fef_params));
   if (R < 1 || R > (1 << 24)) return fail(FEF_ERR_INVALID_ARG, "R = %d out of range [1, 2^24]", R);
   if (prm->V < 1 || prm->d < 1) return fail(FEF_ERR_INVALID_ARG, "V and d must be positive");
+  if (prm->V > kMaxGivenV) return fail(FEF_ERR_INVALID_ARG, "V = %d exceeds 2^29", prm->V);
   if (prm->d % 32 != 0 || prm->d > (1 << 20))
     return fail(FEF_ERR_INVALID_ARG, "a 4-bit head needs d to be a multiple of 32, at most 2^20 (got %d)", prm->d);
   if (prm->dtype != FEF_BF16 && prm->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", prm->dtype);
@@ -603,12 +609,15 @@ fef_status check_edit(const fef_edit_params* p, size_t* total) {
   if (p->struct_size != sizeof(fef_edit_params))
     return fail(FEF_ERR_INVALID_ARG, "struct_size %u does not match this library's %zu", p->struct_size, sizeof(fef_edit_params));
   if (p->B < 1 || p->V < 1) return fail(FEF_ERR_INVALID_ARG, "B and V must be >= 1 (got %d, %d)", p->B, p->V);
+  if (p->V > kMaxGivenV) return fail(FEF_ERR_INVALID_ARG, "V = %d exceeds 2^29", p->V);
   if (p->K < 1 || p->K > FEF_MAX_K) return fail(FEF_ERR_INVALID_ARG, "K = %d out of range [1, %d]", p->K, FEF_MAX_K);
   if ((long)p->B * p->K > (1L << 24)) return fail(FEF_ERR_INVALID_ARG, "B*K = %ld exceeds 2^24 rows per call", (long)p->B * p->K);
   if (p->dtype != FEF_BF16 && p->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
   if (!(p->temperature > 0.f) || !(p->temperature < 1e30f))
     return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number");
   if (p->history_max < 0 || p->n_bias < 0) return fail(FEF_ERR_INVALID_ARG, "history_max and n_bias must not be negative");
+  if (p->history_max > kMaxList || p->n_bias > kMaxList)
+    return fail(FEF_ERR_INVALID_ARG, "history_max = %d and n_bias = %d must not exceed 2^30", p->history_max, p->n_bias);
   if (p->masks != 0 && p->masks != 1 && p->masks != p->K)
     return fail(FEF_ERR_INVALID_ARG, "masks must be 0, 1 or K (got %d)", p->masks);
   for (const int64_t s : {p->seq_stride, p->slot_stride, p->out_seq_stride, p->out_slot_stride})
