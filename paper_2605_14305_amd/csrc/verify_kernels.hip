@@ -107,9 +107,11 @@ struct Found {
   float total;   // sum of all masses
 };
 
-// min{i in [0,n) : sum_{j<=i} mass(j) >= target} over non-negative masses, ascending i.
+// min{i in [0,n) : mass(i) > 0, sum_{j<=i} mass(j) >= target} over non-negative masses, ascending i.
 // Thread t owns the contiguous segment [t*per, (t+1)*per).  If rounding leaves every prefix
 // below the target, the last index with positive mass is returned (index 0 if there is none).
+// Positive, because the sum in order at the end of a segment and the scanned start of the next one differ by roundings: a target
+// between them is reached by the next segment's first element whatever its mass, be it a token that the law does not have or one past n.
 template <class F>
 __device__ inline Found block_find_first(int n, F mass, float target, BlockTmp& t) {
   const int per = (n + NT - 1) / NT;
@@ -123,8 +125,11 @@ __device__ inline Found block_find_first(int n, F mass, float target, BlockTmp& 
   for (int i = begin; i < end; ++i) {
     const float mi = mass(i);
     const float nxt = run + mi;
-    if (mi > 0.f) { last_pos = i; before_pos = run; }
-    if (cand == INT_MAX && nxt >= target) { cand = i; before = run; }
+    if (mi > 0.f) {
+      last_pos = i;
+      before_pos = run;
+      if (cand == INT_MAX && nxt >= target) { cand = i; before = run; }
+    }
     run = nxt;
   }
   int win = block_min_int(cand, t);
@@ -165,8 +170,11 @@ __device__ inline Found wave_find_first(int n, F mass, float target) {
   for (int i = begin; i < end; ++i) {
     const float mi = mass(i);
     const float nxt = run + mi;
-    if (mi > 0.f) { last_pos = i; before_pos = run; }
-    if (cand == INT_MAX && nxt >= target) { cand = i; before = run; }
+    if (mi > 0.f) {
+      last_pos = i;
+      before_pos = run;
+      if (cand == INT_MAX && nxt >= target) { cand = i; before = run; }
+    }
     run = nxt;
   }
   int win = wave_min_int(cand);
@@ -202,8 +210,11 @@ __device__ inline Found wave_find_first_reg(const float (&m)[PER], float target)
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const float nxt = run + m[j];
-    if (m[j] > 0.f) { last_pos = j; before_pos = run; }
-    if (cand < 0 && nxt >= target) { cand = j; before = run; }
+    if (m[j] > 0.f) {
+      last_pos = j;
+      before_pos = run;
+      if (cand < 0 && nxt >= target) { cand = j; before = run; }
+    }
     run = nxt;
   }
   // segments ascend with the lane id: the lowest lane that reached the target holds the answer
@@ -241,24 +252,28 @@ __device__ inline int window_slot(const VerifyArgs& a, int b, int m, int& unreso
   return wave_max_int(pos);
 }
 
+// First token of a tile whose logit is the tile's maximum.  Every partial maximum is the exact maximum of the stored logits of its
+// tile.  Whole wavefront.
+__device__ inline int tile_argmax(const VerifyArgs& a, const float* L, int tile, float tile_max) {
+  const int lane = threadIdx.x & 63;
+  const int v0 = tile_start(a, tile);
+  const int nv = min(tile_start(a, tile + 1), a.V) - v0;
+  int cand = INT_MAX;
+  for (int i = lane; i < nv && cand == INT_MAX; i += kWave)
+    if (L[v0 + i] == tile_max) cand = i;
+  const int idx = wave_min_int(cand);
+  return idx == INT_MAX ? v0 : v0 + idx;
+}
+
 // Greedy variant: arg max of a logits row (lowest token id on a tie) from the head kernel's
-// partials.  Every partial maximum is the exact maximum of the stored logits of its tile, so the
-// first tile whose maximum equals the row maximum holds the answer, and the first token of that
-// tile whose stored logit equals it is the arg max.  Whole wavefront.
+// partials: the first tile whose maximum equals the row maximum holds the answer.  Whole wavefront.
 __device__ inline int row_argmax(const VerifyArgs& a, const float2* P, const float* L, float row_max) {
   const int lane = threadIdx.x & 63;
   int cand = INT_MAX;
   for (int t = lane; t < a.nT && cand == INT_MAX; t += kWave)
     if (P[t].x == row_max) cand = t;
   const int tile = wave_min_int(cand);
-  if (tile == INT_MAX) return 0;  // only if the row holds NaN
-  const int v0 = tile_start(a, tile);
-  const int nv = min(tile_start(a, tile + 1), a.V) - v0;
-  cand = INT_MAX;
-  for (int i = lane; i < nv && cand == INT_MAX; i += kWave)
-    if (L[v0 + i] == row_max) cand = i;
-  const int idx = wave_min_int(cand);
-  return idx == INT_MAX ? v0 : v0 + idx;
+  return tile == INT_MAX ? 0 : tile_argmax(a, L, tile, row_max);  // no such tile only if the row holds NaN
 }
 
 constexpr int kChunkPer = 16;  // residual chunks per lane in the one-wavefront final phase
@@ -423,7 +438,8 @@ __device__ __forceinline__ void row_lse_draft(const VerifyArgs& a, int r, const 
       } else {
         in = wave_find_first(nv, [&](int i) { return expf(L[v0 + i] - lse); }, u - tile.before);
       }
-      x = v0 + in.idx;
+      // a tile may hold a mass whose tokens' own are too small for a number
+      x = in.total == 0.f ? tile_argmax(a, L, tile.idx, P[tile.idx].x) : v0 + in.idx;
     }
   }
   if (lane == 0) {
