@@ -328,8 +328,10 @@ fef_status fef_edit_logits(const fef_edit_params* prm, const void* logits, float
  * edits know the drafts as their prefix), and a TARGET call verifies; the draft rows stay as they were in between.
  *   logits  [2, B, K, ld] device float, 16-byte aligned, ld a multiple of 64 and at least V: draft rows, then target rows, already
  *           divided by the temperature.  -inf marks a token that a law does not have; columns from V on are read but ignored.  A row
- *           of nothing but -inf is no law: a slot with such a row is rejected (the greedy variant takes the row for token 0), and
- *           its token, in [0, V) and with a confidence that may be NaN, means nothing
+ *           of nothing but -inf, or one with a +inf or a NaN, is no law: its tokens have no mass, and a slot with such a row is
+ *           rejected (the greedy variant compares arg maxes, that of a row without a logit above -inf being token 0, that of one with a
+ *           NaN some token).  Over such a draft row the slot's token is drawn from the target law itself.  Over such a target row it is
+ *           the row's arg max, with a confidence of 0; to force a token, mask all others instead of raising it to +inf
  * Fields of prm that are read: as in fef_verify_step but for d, dtype, temperature, gemm_variant; V is at most 2^29, ev_head_begin and ev_head_end
  * must be NULL.  Workspace: fef_verify_logits_workspace_bytes (0 if the arguments are invalid). */
 size_t fef_verify_logits_workspace_bytes(const fef_params* prm, int32_t K, int32_t block);

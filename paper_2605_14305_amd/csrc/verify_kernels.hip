@@ -235,6 +235,11 @@ __device__ inline Found wave_find_first_reg(const float (&m)[PER], float target)
   return f;
 }
 
+// A row is no law if nothing of it is above -inf, or if +inf or NaN is among it: then its log-sum-exp is no finite number and its tokens
+// have no mass (so that a residual over such a draft row is the target law itself).  mass_lse: +inf in place of such a log-sum-exp.
+__device__ inline float mass_lse(float lse) { return fabsf(lse) < INFINITY ? lse : INFINITY; }
+__device__ inline float token_mass(float logit, float lse) { return lse < INFINITY ? expf(logit - lse) : 0.f; }
+
 // window slot m = (m+1)-th unresolved position of block b in ascending order; also counts the
 // unresolved positions.  Whole wavefront.
 __device__ inline int window_slot(const VerifyArgs& a, int b, int m, int& unresolved) {
@@ -573,7 +578,8 @@ __global__ __launch_bounds__(NT) void logit_partials_kernel(VerifyArgs a, int ro
 #pragma unroll
     for (int j = 0; j < 4; ++j) e += __builtin_amdgcn_exp2f((l[i][j] - mx) * kLog2e);
     e = wave_sum(e);
-    if (lane == 0) const_cast<float2*>(a.partials)[(size_t)(row + r) * a.nT + t] = make_float2(mx, e);
+    // (a NaN would leave the row a law over the other tiles: with an infinite maximum it has none)
+    if (lane == 0) const_cast<float2*>(a.partials)[(size_t)(row + r) * a.nT + t] = make_float2(e == e ? mx : INFINITY, e);
   }
 }
 
@@ -647,7 +653,7 @@ __device__ void finalize_sequence(const VerifyArgs& a, int b, const SeqState& st
     const float u = tmp.bcast_u;
     if (a.greedy) {
       z = st.rej_xtarget;  // residual of two point masses: the target's
-      z_conf = expf(Lp[z] - lse_p);
+      z_conf = token_mass(Lp[z], lse_p);
     } else if (a.nRC <= kWave * kChunkPer) {
       // one wavefront, everything in registers
       if (tid < kWave) {
@@ -675,8 +681,8 @@ __device__ void finalize_sequence(const VerifyArgs& a, int b, const SeqState& st
           float rv[4], pe[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            pe[j] = expf(pv[j] - lse_p);
-            rv[j] = v0 + j < a.V ? fmaxf(pe[j] - expf(qv[j] - lse_q), 0.f) : 0.f;
+            pe[j] = token_mass(pv[j], lse_p);
+            rv[j] = v0 + j < a.V ? fmaxf(pe[j] - token_mass(qv[j], lse_q), 0.f) : 0.f;
           }
           const Found in = wave_find_first_reg<4>(rv, u * chunk.total - chunk.before);
           zz = chunk.idx * kResidChunk + in.idx;
@@ -695,7 +701,7 @@ __device__ void finalize_sequence(const VerifyArgs& a, int b, const SeqState& st
           const float gbest = wave_max(best);
           zz = wave_min_int(best == gbest ? bi : INT_MAX);
           if (zz == INT_MAX) zz = 0;  // no logit above -inf
-          zc = expf(Lp[zz] - lse_p);
+          zc = token_mass(Lp[zz], lse_p);
         }
         if (tid == 0) { tmp.bcast_i = zz; tmp.bcast_f = zc; }
       }
@@ -719,7 +725,7 @@ __device__ void finalize_sequence(const VerifyArgs& a, int b, const SeqState& st
       const Found in = block_find_first(
           nv,
           [&](int i) {
-            return fmaxf(expf(Lp[v0 + i] - lse_p) - expf(Lq[v0 + i] - lse_q), 0.f);
+            return fmaxf(token_mass(Lp[v0 + i], lse_p) - token_mass(Lq[v0 + i], lse_q), 0.f);
           },
           target - chunk.before, tmp);
       z = v0 + in.idx;
@@ -735,7 +741,7 @@ __device__ void finalize_sequence(const VerifyArgs& a, int b, const SeqState& st
       z = block_min_int(best == gbest ? bi : INT_MAX, tmp);
       if (z == INT_MAX) z = 0;  // no logit above -inf
     }
-    z_conf = expf(Lp[z] - lse_p);
+    z_conf = token_mass(Lp[z], lse_p);
     }
   }
 
@@ -827,16 +833,15 @@ __device__ inline void accept_tests(const VerifyArgs& a, int b, SeqState& st) {
   const int xt = a.greedy ? a.xtarget[sl] : -1;
   bool rejected = false;
   if (lane < window) {
-    const float lq = a.logits[(size_t)sl * a.ldl + x] - lse_q;
-    const float lp = a.logits[(size_t)(BK + sl) * a.ldl + x] - lse_p;
-    const float ratio = expf(lp - lq);
+    const float logit_p = a.logits[(size_t)(BK + sl) * a.ldl + x];
+    const float ratio = expf(logit_p - lse_p - (a.logits[(size_t)sl * a.ldl + x] - lse_q));
     const float u = philox_uniform(a.seed, a.pos_base + (uint32_t)pos, a.step,
                                    a.seq_base + (uint32_t)b, kStreamAccept);
     // greedy: the ratio of the two point masses is 1 if the arg maxes agree, else 0
     // (u < 1, so this is u <= min(1, ratio); a row without a law makes the ratio NaN, which is a rejection)
     rejected = a.greedy ? x != xt : !(ratio >= 1.f || u <= ratio);
     st.x[lane] = x;
-    st.ptok[lane] = expf(lp);
+    st.ptok[lane] = token_mass(logit_p, mass_lse(lse_p));
   }
   const unsigned long long rej = __ballot(rejected);
   const int acc = rej ? __ffsll((long long)rej) - 1 : window;
@@ -845,8 +850,8 @@ __device__ inline void accept_tests(const VerifyArgs& a, int b, SeqState& st) {
     st.acc_len = acc;
   }
   if (lane == acc && acc < window) {  // the rejected slot's own values, for the final phase
-    st.rej_lse_q = lse_q;
-    st.rej_lse_p = lse_p;
+    st.rej_lse_q = mass_lse(lse_q);
+    st.rej_lse_p = mass_lse(lse_p);
     st.rej_pos = pos;
     st.rej_xtarget = xt;
   }
@@ -879,13 +884,13 @@ __device__ inline Quad load_quad(const VerifyArgs& a, const float* Lq, const flo
   }
   return r;
 }
-// Residual mass (and, if asked for, overlap mass) of a chunk whose four tokens from v on this lane holds.
+// Residual mass (and, if asked for, overlap mass) of a chunk whose four tokens from v on this lane holds; log-sum-exps from mass_lse.
 __device__ inline float chunk_mass(const VerifyArgs& a, const Quad& x, int v, float lse_q, float lse_p, float* overlap) {
   float rs = 0.f, as = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if (v + j < a.V) {
-      const float q = expf(x.q[j] - lse_q), p = expf(x.p[j] - lse_p);
+      const float q = token_mass(x.q[j], lse_q), p = token_mass(x.p[j], lse_p);
       rs += fmaxf(p - q, 0.f);
       as += fminf(p, q);
     }
@@ -937,7 +942,7 @@ __device__ __forceinline__ void slot_masses(const VerifyArgs& a, int s, int c0) 
   const float* Lq = a.logits + (size_t)s * a.ldl;
   const float* Lp = a.logits + (size_t)(BK + s) * a.ldl;
   const int window = a.window[s / a.K];
-  const float lse_q = a.lse[s], lse_p = a.lse[BK + s];
+  const float lse_q = mass_lse(a.lse[s]), lse_p = mass_lse(a.lse[BK + s]);
   Quad x[kMassPer];
 #pragma unroll
   for (int j = 0; j < kMassPer; ++j) x[j] = load_quad<true>(a, Lq, Lp, (c0 + j) * kResidChunk + lane * 4);
