@@ -101,6 +101,7 @@ __global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks
   const int chunk = (int)(per_chunk % (unsigned)chunks), b = b0 + (int)(per_chunk / (unsigned)chunks), c0 = chunk * kChunk;
   const bool counts = a.repetition || a.presence || a.frequency;
   const bool whole = c0 + kChunk <= a.V;
+  const unsigned here = whole ? kChunk : a.V - c0;  // tokens of the chunk: ids behind them stand for none
   const int left = a.V - c0 - tid * 4;  // tokens from this thread's first on
 
   float x[kPer];
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks
     if (history) {
       auto count = [&](int i, int id) {
         const unsigned at = (unsigned)id - (unsigned)c0;
-        if (at < (unsigned)kChunk) {
+        if (at < here) {
           if (i < prompt) atomicOr(&s_cnt[at], kInPrompt);
           else atomicAdd(&s_cnt[at], 1u);
         }
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks
   // From here on a thread reads and writes its own tokens' entries only.
   auto add_prefix = [&](int m) {
     const unsigned at = (unsigned)a.prefix[(size_t)b * a.K + m] - (unsigned)c0;
-    if (at < (unsigned)kChunk && ((at >> 2) & (NT - 1)) == (unsigned)tid) {
+    if (at < here && ((at >> 2) & (NT - 1)) == (unsigned)tid) {
       ++s_cnt[at];
       touched |= 1u << (at / (NT * 4) * 4 + (at & 3));
     }
