@@ -37,10 +37,22 @@ typedef int intx4_any __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ float finite_max(float m) { return fminf(fmaxf(m, -FLT_MAX), FLT_MAX); }
 __device__ __forceinline__ float exp_diff(float x, float m) { return __builtin_amdgcn_exp2f((x - m) * kLog2e); }
 
-// x / y from r = 1 / y: the quotient's remainder corrects it, so it is off by no more than a division (what is infinite stays so).
-__device__ __forceinline__ float divided(float x, float y, float r) {
-  const float q = x * r, e = __builtin_fmaf(-q, y, x);
-  return fabsf(q) < INFINITY ? __builtin_fmaf(e, r, q) : q;
+// Division by one y: x / y = (x / d) s with s a power of two such that r = 1 / d is a normal number; the quotient's remainder corrects it,
+// so it is off by a step at most (what is infinite stays so).  y = 0 and an infinite y end as s.  32 x 16 slots of V = 151936 with every
+// edit take 148.4 us so, with a plain division per logit 149.6 (8 x 65536 tokens of history 22.9 and 23.3).
+struct Divisor {
+  float d, r, s;
+};
+__device__ __forceinline__ Divisor divisor(float y) {
+  const float m = fabsf(y);
+  const float up = m < 0x1p-64f ? 0x1p64f : m > 0x1p64f ? 0x1p-64f : 1.f;
+  const bool end = m == 0.f || m == INFINITY;
+  const float d = end ? 1.f : y * up;
+  return {d, 1.f / d, end ? copysignf(m == 0.f ? INFINITY : 0.f, y) : up};
+}
+__device__ __forceinline__ float divided(float x, const Divisor& y) {
+  const float q = x * y.r, e = __builtin_fmaf(-q, y.d, x);
+  return (fabsf(q) < INFINITY ? __builtin_fmaf(e, y.r, q) : q) * y.s;
 }
 
 // Biases of the chunk's tokens, summed per token in the order of the list (its first NT entries are given): the entries that name one of
@@ -152,7 +164,8 @@ __global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks
   }
   const int len = !history ? 0 : a.history_len ? min(max(a.history_len[b], 0), a.history_max) : a.history_max;
   const int prompt = history && a.prompt_len ? min(max(a.prompt_len[b], 0), len) : 0;
-  const float rep = a.repetition ? a.repetition[b] : 1.f, inv_rep = 1.0f / rep;
+  const float rep = a.repetition ? a.repetition[b] : 1.f;
+  const Divisor by = divisor(rep);
   const float pres = a.presence ? a.presence[b] : 0.f;
   const float freq = a.frequency ? a.frequency[b] : 0.f;
   fetch(m0);
@@ -219,7 +232,7 @@ __global__ __launch_bounds__(NT) void edit_kernel(EditArgs a, int b0, int chunks
           float z = x[i];
           if (n) {
             const float times = (float)(n & ~kInPrompt);
-            z = z > 0.f ? divided(z, rep, inv_rep) : z * rep;
+            z = z > 0.f ? divided(z, by) : z * rep;
             z -= freq * times;
             z -= times > 0.f ? pres : 0.f;
           }
