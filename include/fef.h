@@ -271,7 +271,7 @@ fef_status fef_head_cross_entropy(const fef_params* prm, const void* h, const vo
  *   out_logits [R, ld]     device float, 4-byte aligned, ld >= V; columns from V on are not touched
  * w and bf16 hidden states are exact in the multiply, float32 ones too (taken as three bf16 parts; what lies below 2^-133 is lost);
  * sums are held in 32 bits, in an order that the sizes decide.
- * Fields of prm that are read: struct_size, d (a positive multiple of 32, at most 2^20), V (at most 2^29), dtype, temperature, stream, ev_head_begin /
+ * Fields of prm that are read: struct_size, d (a positive multiple of 32, at most 2^20), V (at most 2^29), dtype, temperature (1 / tau finite), stream, ev_head_begin /
  * ev_head_end (around the kernel).  1 <= R <= 2^24.  No workspace.  Same conventions and error behaviour as fef_verify_step. */
 fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* codes, const uint8_t* scales, int32_t R,
                           float* out_logits, int64_t ld);
@@ -289,7 +289,7 @@ typedef struct {
   uint32_t struct_size;        /* = sizeof(fef_edit_params)                                        */
   int32_t B, K, V;             /* sequences, window slots (<= FEF_MAX_K), vocabulary (<= 2^29)     */
   int32_t dtype;               /* fef_dtype of the logits                                          */
-  float temperature;           /* tau > 0                                                          */
+  float temperature;           /* tau > 0, 1 / tau finite                                          */
   int64_t seq_stride;          /* elements from a sequence's logits to the next one's, >= 0        */
   int64_t slot_stride;         /* elements from a slot's logits to the next one's, >= 0            */
   int64_t out_seq_stride;      /* the same of the output; rows of the output must not overlap      */

@@ -539,6 +539,9 @@ namespace {
 // one step further, then stay in 32 bits with their sign, and a grid of 16-token tiles below 2^32 threads.
 constexpr int kMaxGivenV = 1 << 29, kMaxList = 1 << 30;
 
+// Logits are multiplied by 1 / tau, which is infinite for tau below 2^-128 (and a logit of 0 would become NaN).
+bool scales_logits(float tau) { return tau > 0.f && tau < 1e30f && 1.f / tau < INFINITY; }
+
 // A call on given logits as one of a 256-token head: a partial per tile, whatever made the logits.
 fef_status logits_params(const fef_params* prm, fef_params* p) {
   if (!prm) return fail(FEF_ERR_INVALID_ARG, "params is NULL");
@@ -582,8 +585,7 @@ fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* c
   if (prm->d % 32 != 0 || prm->d > (1 << 20))
     return fail(FEF_ERR_INVALID_ARG, "a 4-bit head needs d to be a multiple of 32, at most 2^20 (got %d)", prm->d);
   if (prm->dtype != FEF_BF16 && prm->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", prm->dtype);
-  if (!(prm->temperature > 0.f) || !(prm->temperature < 1e30f))
-    return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number");
+  if (!scales_logits(prm->temperature)) return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number with a finite reciprocal");
   if (!h || !codes || !scales || !out_logits) return fail(FEF_ERR_INVALID_ARG, "h, codes, scales and out_logits must not be NULL");
   if (((uintptr_t)h | (uintptr_t)codes | (uintptr_t)scales) & 15)
     return fail(FEF_ERR_INVALID_ARG, "h, codes and scales must be 16-byte aligned");
@@ -613,8 +615,7 @@ fef_status check_edit(const fef_edit_params* p, size_t* total) {
   if (p->K < 1 || p->K > FEF_MAX_K) return fail(FEF_ERR_INVALID_ARG, "K = %d out of range [1, %d]", p->K, FEF_MAX_K);
   if ((long)p->B * p->K > (1L << 24)) return fail(FEF_ERR_INVALID_ARG, "B*K = %ld exceeds 2^24 rows per call", (long)p->B * p->K);
   if (p->dtype != FEF_BF16 && p->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
-  if (!(p->temperature > 0.f) || !(p->temperature < 1e30f))
-    return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number");
+  if (!scales_logits(p->temperature)) return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number with a finite reciprocal");
   if (p->history_max < 0 || p->n_bias < 0) return fail(FEF_ERR_INVALID_ARG, "history_max and n_bias must not be negative");
   if (p->history_max > kMaxList || p->n_bias > kMaxList)
     return fail(FEF_ERR_INVALID_ARG, "history_max = %d and n_bias = %d must not exceed 2^30", p->history_max, p->n_bias);

@@ -51,3 +51,13 @@ def test_round_up_to_the_limit():
     p = fb.make_params(1, 64, 2 ** 29)
     p.workspace, p.workspace_bytes = 0x10000, 16
     assert fb.lib().fef_verify_logits(ctypes.byref(p), 0x1000, 2 ** 29, 1, 1, 0, 0x1000, 0x1000, 0x1000) == fb.FEF_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("tau", [1e-45, 1e-40, 2.9e-39])
+def test_a_temperature_without_a_reciprocal(tau):
+    """1 / tau would be infinite, and a logit of 0 NaN."""
+    assert fb.lib().fef_edit_logits(ctypes.byref(_edit(temperature=tau)), 0x1000, 0x2000, 0x3000) == fb.FEF_ERR_INVALID_ARG
+    assert "reciprocal" in fb.fef_last_error()
+    p = fb.make_params(1, 32, 100, temperature=tau)
+    assert fb.lib().fef_mx4_logits(p, 0x1000, 0x1000, 0x1000, 1, 0x1000, 100) == fb.FEF_ERR_INVALID_ARG
+    assert "reciprocal" in fb.fef_last_error()
