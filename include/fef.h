@@ -188,7 +188,9 @@ size_t fef_workspace_bytes(const fef_params* prm, int32_t K, int32_t block);
  *   out_accept_len  [B]        device int32: accepted drafts a in [0, b]; committed
  *                              positions are min(a+1, b)
  *   out_remask      [B, block] device uint8: unresolved positions after the round
- * Rows of h_* for slots beyond a sequence's window are read but ignored. */
+ * Rows of h_* for slots beyond a sequence's window are read but ignored.
+ * A row of h_* that holds a NaN makes no law, and its slot is rejected (not greedy): over such a draft row the token is drawn from the
+ * target law, over such a target row it is some token of [0, V) with a confidence of 0. */
 fef_status fef_verify_step(const fef_params* prm, const void* h_draft, const void* h_target,
                            const void* W_vocab, int32_t K, int32_t block, uint64_t seed,
                            int32_t* out_tokens, int32_t* out_accept_len, uint8_t* out_remask);
