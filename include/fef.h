@@ -269,7 +269,8 @@ fef_status fef_head_cross_entropy(const fef_params* prm, const void* h, const vo
  *   h          [R, d]      device, dtype prm->dtype (bf16 or f32), 16-byte aligned
  *   codes      [V, d / 2]  device bytes, 16-byte aligned: two e2m1 codes each, the low nibble is the even k; a code is a sign bit
  *                          over the magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6
- *   scales     [V, d / 32] device bytes, 16-byte aligned: e8m0, one power of two per 32 codes; 255 is NaN and makes its token's logits NaN
+ *   scales     [V, d / 32] device bytes, 16-byte aligned: e8m0, one power of two per 32 codes; 255 is NaN and makes its token's logits NaN;
+ *                          weights of 2^128 and more (the larger codes with 253 or 254) are infinite
  *   out_logits [R, ld]     device float, 4-byte aligned, ld >= V; columns from V on are not touched
  * w and bf16 hidden states are exact in the multiply, float32 ones too (taken as three bf16 parts; what lies below 2^-133 is lost);
  * sums are held in 32 bits, in an order that the sizes decide.

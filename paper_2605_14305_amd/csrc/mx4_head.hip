@@ -1,7 +1,7 @@
 // Logits of the vocabulary head from weights in 4 bits (OCP MX, MXFP4): logits[r, v] = inv_tau sum_k h[r, k] w[v, k],
 // w[v, k] = e2m1(code) 2^(scale - 127) with a scale per 32 codes.
 //
-// Numbers.  A code times its scale has two significant bits, so it is exact in bf16, and v_cvt_scalef32_pk_bf16_fp4 makes two of
+// Numbers.  A code times its scale has two significant bits, so below 2^128 it is exact in bf16 (from there on infinite), and v_cvt_scalef32_pk_bf16_fp4 makes two of
 // them with their scale in one instruction (checked over all codes and scales: exact, subnormals too, scale 255 gives NaN).  The
 // products run on v_mfma_f32_16x16x32_bf16 with float32 sums.  The scaled 8-bit multiplies would take the codes as they are, but add
 // with 13 to 15 bits only (measured: error 2^-13.5 of the sum of magnitudes), and two of them per bf16 value cost as much time.
@@ -264,8 +264,9 @@ __global__ __launch_bounds__(kThreads, 2) void mx4_stages_kernel(Mx4Args a, int 
 // Few slices mean few barriers and few partial sums, but every tile of a stage brings its copy of h into registers before the first
 // multiply: one slice wherever h fits (8 rows of d = 512, V = 126464: 11.1 us, in two slices 13.1, in four 16.0), and of more
 // slices the fewest that leave a workgroup eight stages (8 rows of d = 2048, V = 50257 in four slices, six stages: 15.9, in eight 14.7;
-// 16 float32 rows, whose h is three times as long, of d = 1024, V = 32000 in two slices, two stages: 18.1, in eight 11.7), but none that
-// gets no column (8 rows of d = 256, V = 32000 in two slices 5.8, in eight, six of them empty, 8.7).
+// 16 float32 rows, whose h is three times as long, of d = 1024, V = 32000 in two slices, two stages: 18.1, in eight 11.7), but no more
+// slices than units of 128 columns, rounded up to a power of two (8 rows of d = 256, V = 32000 in two slices 5.8, in eight, six of them
+// empty, 8.7; five to seven units in eight slices leave up to three of them empty).
 template <int MT, bool F32>
 bool launch_stages(const Mx4Args& a) {
   const int tiles = (a.V + 15) / 16, nu = (a.d + 127) / 128;
