@@ -885,12 +885,20 @@ __device__ inline Quad load_quad(const VerifyArgs& a, const float* Lq, const flo
   return r;
 }
 // Residual mass (and, if asked for, overlap mass) of a chunk whose four tokens from v on this lane holds; log-sum-exps from mass_lse.
-__device__ inline float chunk_mass(const VerifyArgs& a, const Quad& x, int v, float lse_q, float lse_p, float* overlap) {
+__device__ inline float chunk_mass(const VerifyArgs& a, Quad x, int v, float lse_q, float lse_p, float* overlap) {
+  // a row without a law: one branch for the masses of its tokens, exp(-inf) = 0 (a call with the masses of 64 x 16 slots of V = 126464 1755 to
+  // 1761 us; with a choice per token 1757 to 1767, and 1753 to 1756 where such rows were not looked at)
+  if (!(lse_q < INFINITY))
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.q[j] = -INFINITY;
+  if (!(lse_p < INFINITY))
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.p[j] = -INFINITY;
   float rs = 0.f, as = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if (v + j < a.V) {
-      const float q = token_mass(x.q[j], lse_q), p = token_mass(x.p[j], lse_p);
+      const float q = expf(x.q[j] - lse_q), p = expf(x.p[j] - lse_p);
       rs += fmaxf(p - q, 0.f);
       as += fminf(p, q);
     }
