@@ -330,7 +330,7 @@ fef_status fef_edit_logits(const fef_edit_params* prm, const void* logits, float
  * and options included.  In the method's order a DRAFT call draws the tokens from the draft rows, the caller makes the target rows (whose
  * edits know the drafts as their prefix), and a TARGET call verifies; the draft rows stay as they were in between.
  *   logits  [2, B, K, ld] device float, 16-byte aligned, ld a multiple of 64 and at least V: draft rows, then target rows, already
- *           divided by the temperature.  -inf marks a token that a law does not have; columns from V on are read but ignored.  A row
+ *           divided by the temperature.  -inf, or any number below -2e38, marks a token that a law does not have; columns from V on are read but ignored.  A row
  *           of nothing but -inf, or one with a +inf or a NaN, is no law: its tokens have no mass, and a slot with such a row is
  *           rejected (the greedy variant compares arg maxes, that of a row without a logit above -inf being token 0, that of one with a
  *           NaN some token).  Over such a draft row the slot's token is drawn from the target law itself.  Over such a target row it is

@@ -12,7 +12,7 @@
 // threads arrive.
 //
 // Bound: the read and the write of the logits (32 x 16 slots of V = 151936, 622 MB: 131 us without any edit, 4.7 TB/s, a plain copy of as
-// much 121 to 130; with penalties, biases and masks 148, the edits' instructions), in small calls the way through the tables and the
+// much 121 to 130; with penalties, biases and masks 144 to 149, the edits' instructions), in small calls the way through the tables and the
 // second launch (8 slots of V = 126464: 7.6 and 2 us).  Counting the history again for every chunk beats a table in memory, which would have to
 // be cleared and needs atomics across XCDs.  Stores are non-temporal: grammar masks alone on 128 rows of V = 126464 37 -> 28 us.
 //

@@ -547,7 +547,7 @@ __global__ __launch_bounds__(kSumThreads) void row_sums_draft_kernel(VerifyArgs 
 
 // ---------------------------------------------------------------------------------------------
 // In front of kernel 1 where the caller brings the logits: (max, sum exp) of each row's 256-token tiles, a wavefront per two tiles, four
-// tokens of each per lane, both loads in flight.  Bound: one read of the logits (1024 rows of V = 151936, 622 MB, in 109 us, 5.7 TB/s; a
+// tokens of each per lane, both loads in flight.  Bound: one read of the logits (1024 rows of V = 151936, 622 MB, in 94 to 109 us, 5.7 to 6.6 TB/s; a
 // whole round on them 121 us, with one tile per wavefront 147, with four 127; on 16 rows of V = 126464 16.0, 18.0, 16.3).
 // ---------------------------------------------------------------------------------------------
 constexpr int kPartialTiles = 2;
@@ -838,8 +838,10 @@ __device__ inline void accept_tests(const VerifyArgs& a, int b, SeqState& st) {
     const float u = philox_uniform(a.seed, a.pos_base + (uint32_t)pos, a.step,
                                    a.seq_base + (uint32_t)b, kStreamAccept);
     // greedy: the ratio of the two point masses is 1 if the arg maxes agree, else 0
-    // (u < 1, so this is u <= min(1, ratio); a row without a law makes the ratio NaN, which is a rejection)
-    rejected = a.greedy ? x != xt : !(ratio >= 1.f || u <= ratio);
+    // (u < 1, so this is u <= min(1, ratio); a token that neither law has makes it NaN.  A row without a law rejects by itself: the ratio over a
+    // target row of logits that count as -inf and yet are numbers would be infinite)
+    const bool laws = fabsf(lse_q) < INFINITY && fabsf(lse_p) < INFINITY;
+    rejected = a.greedy ? x != xt : !(laws && (ratio >= 1.f || u <= ratio));
     st.x[lane] = x;
     st.ptok[lane] = token_mass(logit_p, mass_lse(lse_p));
   }
