@@ -13,8 +13,8 @@ gradients of sum_r g[r] ce[r] in h and w.
 
 "adamw": one step t over a list of tensors, with g the gradient: m <- b1 m + (1 - b1) g, v <- b2 v + (1 - b2) g^2,
 p <- p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps), where p is a float32 copy of bf16 parameters if there is one.
-States in 8 bits hold m and sqrt(v) of 256 elements at a time as e4m3 codes under one float32 scale, the largest magnitude / 448, and a
-positive sqrt(v) never becomes 0.
+States in 8 bits hold m and sqrt(v) of 256 elements at a time as e4m3 codes under one float32 scale, the largest magnitude / 448 (0 for
+one below 2^-100), and a positive sqrt(v) never becomes 0 under a scale.
 """
 import math
 
@@ -100,6 +100,7 @@ def _coded(x, positive):
     """e4m3 codes of x and the scales of its blocks of 256."""
     rows = _blocks(x)
     top = rows.abs().amax(1)
+    top = torch.where(top < 2.0 ** -100, torch.zeros_like(top), top)
     y = rows * torch.where(top > 0, 448.0 / top, torch.zeros_like(top))[:, None]
     if positive:
         y = torch.where((rows > 0) & (y < 2.0 ** -9), torch.full((), 2.0 ** -9, device=x.device), y)
