@@ -58,7 +58,7 @@ extern "C" {
 
 #define FEF_MAX_K 64
 #define FEF_MAX_BLOCK 4096
-#define FEF_ABI_VERSION 11
+#define FEF_ABI_VERSION 12
 #define FEF_STATIC_SCRATCH_BYTES (32u << 20) /* built-in scratch of fef_verify_step_static        */
 
 typedef enum {
@@ -340,6 +340,56 @@ fef_status fef_edit_logits(const fef_edit_params* prm, const void* logits, float
 size_t fef_verify_logits_workspace_bytes(const fef_params* prm, int32_t K, int32_t block);
 fef_status fef_verify_logits(const fef_params* prm, const float* logits, int64_t ld, int32_t K, int32_t block, uint64_t seed,
                              int32_t* out_tokens, int32_t* out_accept_len, uint8_t* out_remask);
+
+/* One AdamW step over a list of tensors (the step of Algorithm 1 after the gradients).  For every element, with g its gradient times
+ * *grad_scale, and p its float32 copy `master` where there is one, else the parameter:
+ *   m <- beta1 m + (1 - beta1) g
+ *   v <- beta2 v + (1 - beta2) g^2
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in float32, each operation rounded once, in this order (the constants are computed in 64 bits and rounded: 1 - beta1, 1 - beta2,
+ * lr / (1 - beta1^t) as the rounded lr times the rounded 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)); a bf16 parameter is p rounded to nearest.
+ * Without `master`, steps of a bf16 parameter below half its last bit are lost.
+ * States in 8 bits (FEF_STATE_E4M3) hold m and sqrt(v): codes in OCP e4m3, 256 consecutive elements under one float32 scale, the largest
+ * magnitude of the 256 / 448, each rounded to nearest.  A positive sqrt(v) that would round to 0 takes the smallest code.  A block whose
+ * largest magnitude is below 2^-100 is held as zeros.  Codes and scales that start at zero are the states of step 1.  A code moves only
+ * when an element changes by half a code step, 3 to 6 %, against the largest of its block; the scale follows exactly.
+ * A gradient that is no finite number makes its element's p, m and v NaN or infinite, in 8 bits its whole block of states. */
+typedef enum {
+  FEF_STATE_F32 = 0, /* m and v float32 [n]                                                          */
+  FEF_STATE_E4M3 = 1 /* m and v bytes [n], m_scale and v_scale float32 [ceil(n / 256)]                */
+} fef_state_dtype;
+
+typedef struct {
+  void* param;          /* [n], dtype                                                              */
+  const void* grad;     /* [n], grad_dtype                                                         */
+  float* master;        /* [n] float32 copy of a bf16 parameter, which is written from it; or NULL */
+  void* m;              /* [n]                                                                     */
+  void* v;              /* [n]                                                                     */
+  float* m_scale;       /* [ceil(n / 256)], NULL with FEF_STATE_F32                                */
+  float* v_scale;
+  int64_t n;            /* elements, at most 2^36; 0: nothing to do, the pointers are not looked at */
+  double weight_decay;  /* finite, >= 0                                                            */
+} fef_adamw_tensor;
+
+typedef struct {
+  uint32_t struct_size;    /* = sizeof(fef_adamw_params)                                            */
+  int32_t dtype;           /* fef_dtype of the parameters                                           */
+  int32_t grad_dtype;      /* fef_dtype of the gradients                                            */
+  int32_t state_dtype;     /* fef_state_dtype                                                       */
+  double lr;               /* finite                                                                */
+  double beta1, beta2;     /* in [0, 1)                                                             */
+  double eps;              /* finite, > 0 as a float32                                              */
+  int64_t step;            /* t >= 1                                                                */
+  const float* schedule;   /* NULL, or device [3]: lr, 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t), used in place of lr and step (for a
+                              captured graph, whose arguments stay)                                 */
+  const float* grad_scale; /* NULL, or device [1]                                                   */
+  void* stream;            /* hipStream_t; NULL = the null stream                                   */
+} fef_adamw_params;
+
+/* `tensors` (host memory) is read before the call returns.  Addresses are aligned to their elements (16 bytes: faster, with the same
+ * results).  What the call writes may not overlap anything else it reads or writes, within a tensor or between tensors: the same tensor
+ * twice is refused.  count in [0, 65536].  No workspace.  Conventions and error behaviour as in fef_verify_step. */
+fef_status fef_adamw_step(const fef_adamw_params* prm, const fef_adamw_tensor* tensors, int32_t count);
 
 /* Philox4x32-10 word 0 -> uniform, evaluated on the host with the same code the kernels
  * use; lets callers and tests reproduce a draw.  Pure host function. */

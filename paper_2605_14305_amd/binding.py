@@ -21,14 +21,15 @@ FEF_GEMM_AUTO, FEF_GEMM_SKINNY, FEF_GEMM_TILED, FEF_GEMM_F32, FEF_GEMM_TILED256,
 FEF_GEMM_ROWSTREAM = 6
 FEF_MAX_K, FEF_MAX_BLOCK = 64, 4096
 FEF_PHASE_FUSED, FEF_PHASE_DRAFT, FEF_PHASE_TARGET = 0, 1, 2
+FEF_STATE_F32, FEF_STATE_E4M3 = 0, 1
 
-ABI_VERSION = 11   # FEF_ABI_VERSION of include/fef.h this binding's fef_params mirrors
+ABI_VERSION = 12   # FEF_ABI_VERSION of include/fef.h this binding's fef_params mirrors
 
 EXPORTS = ["fef_workspace_bytes", "fef_verify_step", "fef_select_gemm", "fef_uniform",
            "fef_status_string", "fef_last_error", "fef_abi_version", "fef_copy_probe", "fef_read_probe",
            "fef_cross_entropy_workspace_bytes", "fef_head_cross_entropy", "fef_topn_step",
            "fef_verify_step_static", "fef_mx4_logits", "fef_edit_workspace_bytes", "fef_edit_logits",
-           "fef_verify_logits_workspace_bytes", "fef_verify_logits"]
+           "fef_verify_logits_workspace_bytes", "fef_verify_logits", "fef_adamw_step"]
 FEF_STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -80,6 +81,25 @@ class fef_edit_params(ctypes.Structure):
 
 _EDIT_PARAMS_SIZE = ctypes.sizeof(fef_edit_params)
 _PACK_EDIT = struct.Struct("@I4if4qi7Pi2PiPPNP").pack_into  # fef_edit_params, field by field in native alignment
+
+
+class fef_adamw_tensor(ctypes.Structure):
+    _fields_ = [
+        ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("master", ctypes.c_void_p),
+        ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("n", ctypes.c_int64), ("weight_decay", ctypes.c_double),
+    ]
+
+
+class fef_adamw_params(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("state_dtype", ctypes.c_int32),
+        ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+        ("step", ctypes.c_int64),
+        ("schedule", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p),
+        ("stream", ctypes.c_void_p),
+    ]
 
 
 class FefError(RuntimeError):
@@ -144,6 +164,8 @@ def lib():
         L.fef_edit_workspace_bytes.argtypes = [ctypes.POINTER(fef_edit_params)]
         L.fef_edit_logits.restype = ctypes.c_int
         L.fef_edit_logits.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+        L.fef_adamw_step.restype = ctypes.c_int
+        L.fef_adamw_step.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32]
         if L.fef_abi_version() != ABI_VERSION:
             raise RuntimeError(f"{LIB_PATH} has ABI version {L.fef_abi_version()}, this binding needs {ABI_VERSION}: "
                                "rebuild it with `python -m paper_2605_14305_amd.build`")
@@ -558,3 +580,74 @@ class VerifyLogits:
         if s != FEF_OK:
             raise FefError(s, fef_last_error())
         return self.out_tokens, self.out_accept_len, self.out_remask
+
+
+class AdamW:
+    """One AdamW step at a time over a list of parameters (fef_adamw_step), all bf16 or all float32, contiguous.  `grads`: their
+    gradients, all of one of these types.  states "f32" or "8bit" (e4m3 codes and a scale per 256 elements).  `master`: True for float32
+    copies of bf16 parameters, made here, or a list of them.  `weight_decay`: one for all or one for each.  m, v (and m_scale, v_scale)
+    go on from given states; left out, they start at zero.  `schedule` (device float32 [3]: lr, 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t))
+    replaces lr and the step count, `grad_scale` (device float32 [1]) multiplies the gradients.
+    Holds the tensors; their contents may change between steps (a backward pass writes the gradients), the tensors themselves may
+    not be exchanged.  `lr` and `step_count` may be set between steps; a step adds one to `step_count` first."""
+
+    def __init__(self, params, grads, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, states="f32", master=None, m=None, v=None,
+                 m_scale=None, v_scale=None, step=0, schedule=None, grad_scale=None):
+        self.params, self.grads, self.lr, self.step_count = list(params), list(grads), lr, step
+        n = len(self.params)
+        assert n and len(self.grads) == n, "a gradient per parameter"
+        assert states in ("f32", "8bit")
+        self.device = self.params[0].device
+        eight = states == "8bit"
+
+        def made(given, default):
+            out = [default(p) for p in self.params] if given is None or given is True or len(given) == 0 else list(given)
+            assert len(out) == n, "one for each parameter"
+            return out
+
+        def blocks(p):
+            return (p.numel() + 255) // 256
+
+        self.master = made(master, lambda p: p.float()) if master is True or master else None
+        state = torch.float8_e4m3fn if eight else torch.float32
+        self.m = made(m, lambda p: torch.zeros(p.numel(), dtype=torch.uint8 if eight else state, device=p.device).view(state))
+        self.v = made(v, lambda p: torch.zeros(p.numel(), dtype=torch.uint8 if eight else state, device=p.device).view(state))
+        if eight:
+            self.m_scale = made(m_scale, lambda p: torch.zeros(blocks(p), device=p.device))
+            self.v_scale = made(v_scale, lambda p: torch.zeros(blocks(p), device=p.device))
+        else:
+            assert not m_scale and not v_scale, "scales belong to states in 8 bits"
+            self.m_scale = self.v_scale = None
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        assert len(decay) == n, "one weight decay for each parameter"
+        kinds = (torch.bfloat16, torch.float32)
+        assert self.params[0].dtype in kinds and self.grads[0].dtype in kinds
+        assert self.master is None or self.params[0].dtype == torch.bfloat16, "float32 copies are for bf16 parameters"
+        self._tensors = (fef_adamw_tensor * n)()
+        for i, p in enumerate(self.params):
+            count = p.numel()
+            for t, kind, size in ((p, self.params[0].dtype, count), (self.grads[i], self.grads[0].dtype, count),
+                                  (self.master and self.master[i], torch.float32, count), (self.m[i], state, count), (self.v[i], state, count),
+                                  (self.m_scale and self.m_scale[i], torch.float32, blocks(p)),
+                                  (self.v_scale and self.v_scale[i], torch.float32, blocks(p))):
+                assert t is None or (t.dtype == kind and t.numel() == size and t.is_contiguous() and t.device == self.device and t.is_cuda)
+            e = self._tensors[i]
+            e.param, e.grad, e.m, e.v = p.data_ptr(), self.grads[i].data_ptr(), self.m[i].data_ptr(), self.v[i].data_ptr()
+            e.master = _ptr(self.master[i]) if self.master else None
+            e.m_scale, e.v_scale = (self.m_scale[i].data_ptr(), self.v_scale[i].data_ptr()) if eight else (None, None)
+            e.n, e.weight_decay = count, decay[i]
+        for t, size in ((schedule, 3), (grad_scale, 1)):
+            assert t is None or (t.dtype == torch.float32 and t.numel() == size and t.is_contiguous() and t.is_cuda)
+        self.schedule, self.grad_scale = schedule, grad_scale
+        self._params = fef_adamw_params(ctypes.sizeof(fef_adamw_params), FEF_BF16 if self.params[0].dtype == torch.bfloat16 else FEF_F32,
+                                        FEF_BF16 if self.grads[0].dtype == torch.bfloat16 else FEF_F32,
+                                        FEF_STATE_E4M3 if eight else FEF_STATE_F32, lr, betas[0], betas[1], eps, max(step, 1), _ptr(schedule),
+                                        _ptr(grad_scale), None)
+
+    def step(self):
+        p = self._params
+        p.lr, p.step, p.stream = self.lr, self.step_count + 1, _stream(self.device)
+        r = (_lib or lib()).fef_adamw_step(ctypes.byref(p), self._tensors, len(self.params))
+        if r != FEF_OK:
+            raise FefError(r, fef_last_error())
+        self.step_count += 1

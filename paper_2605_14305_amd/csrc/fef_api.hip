@@ -4,7 +4,11 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
+#include <cmath>
+#include <memory>
+#include <new>
 
 #include "../../include/fef.h"
 #include "fef_device.hpp"
@@ -674,6 +678,105 @@ fef_status fef_edit_logits(const fef_edit_params* p, const void* logits, float* 
   a.stream = (hipStream_t)p->stream;
   const hipError_t e = fef::launch_edit(a);
   if (e != hipSuccess) return fail(FEF_ERR_HIP, "edit kernel launch: %s", hipGetErrorString(e));
+  return FEF_OK;
+}
+
+namespace {
+// An address range of an AdamW step; ranges that are written may not meet any other.
+struct Range {
+  uintptr_t begin, end;
+  bool written;
+};
+
+fef_status check_adamw(const fef_adamw_params* p, const fef_adamw_tensor* ts, int32_t count) {
+  if (!p) return fail(FEF_ERR_INVALID_ARG, "params is NULL");
+  if (p->struct_size != sizeof(fef_adamw_params))
+    return fail(FEF_ERR_INVALID_ARG, "struct_size %u does not match this library's %zu", p->struct_size, sizeof(fef_adamw_params));
+  if (count < 0 || count > 65536) return fail(FEF_ERR_INVALID_ARG, "count = %d out of range [0, 65536]", count);
+  if (count > 0 && !ts) return fail(FEF_ERR_INVALID_ARG, "tensors is NULL with count %d", count);
+  if (p->dtype != FEF_BF16 && p->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
+  if (p->grad_dtype != FEF_BF16 && p->grad_dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown grad_dtype %d", p->grad_dtype);
+  if (p->state_dtype != FEF_STATE_F32 && p->state_dtype != FEF_STATE_E4M3)
+    return fail(FEF_ERR_INVALID_ARG, "unknown state_dtype %d", p->state_dtype);
+  if (!(std::fabs(p->lr) <= 1e30)) return fail(FEF_ERR_INVALID_ARG, "lr must be a finite number");
+  if (!(p->beta1 >= 0 && (float)p->beta1 < 1.f) || !(p->beta2 >= 0 && (float)p->beta2 < 1.f))
+    return fail(FEF_ERR_INVALID_ARG, "beta1 and beta2 must lie in [0, 1)");
+  if (!(p->eps <= 1e30) || !((float)p->eps > 0.f)) return fail(FEF_ERR_INVALID_ARG, "eps must be a positive finite number");
+  if (p->step < 1) return fail(FEF_ERR_INVALID_ARG, "step must be at least 1 (got %ld)", (long)p->step);
+  if (((uintptr_t)p->schedule | (uintptr_t)p->grad_scale) & 3)
+    return fail(FEF_ERR_INVALID_ARG, "schedule and grad_scale must be 4-byte aligned");
+  if (count == 0) return FEF_OK;
+  const bool eight = p->state_dtype == FEF_STATE_E4M3;
+  const uintptr_t pa = p->dtype == FEF_BF16 ? 1 : 3, ga = p->grad_dtype == FEF_BF16 ? 1 : 3, sa = eight ? 0 : 3;
+  std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[(size_t)count * 7 + 2]);
+  if (!ranges) return fail(FEF_ERR_UNSUPPORTED, "no host memory for the check of %d tensors", count);
+  size_t used = 0;
+  auto add = [&](const void* at, size_t bytes, bool written) {
+    ranges[used++] = Range{(uintptr_t)at, (uintptr_t)at + bytes, written};
+  };
+  if (p->schedule) add(p->schedule, 12, false);
+  if (p->grad_scale) add(p->grad_scale, 4, false);
+  for (int i = 0; i < count; ++i) {
+    const fef_adamw_tensor& t = ts[i];
+    if (t.n < 0 || t.n > (1L << 36)) return fail(FEF_ERR_INVALID_ARG, "tensor %d: n = %ld out of range [0, 2^36]", i, (long)t.n);
+    if (!(t.weight_decay >= 0 && t.weight_decay <= 1e30)) return fail(FEF_ERR_INVALID_ARG, "tensor %d: weight_decay must be finite and not negative", i);
+    if (t.n == 0) continue;
+    if (!t.param || !t.grad || !t.m || !t.v) return fail(FEF_ERR_INVALID_ARG, "tensor %d: param, grad, m and v must not be NULL", i);
+    if (t.master && p->dtype != FEF_BF16) return fail(FEF_ERR_INVALID_ARG, "tensor %d: master is for bf16 parameters", i);
+    if (eight ? !t.m_scale || !t.v_scale : t.m_scale || t.v_scale)
+      return fail(FEF_ERR_INVALID_ARG, "tensor %d: m_scale and v_scale belong to states in 8 bits", i);
+    if (((uintptr_t)t.param & pa) || ((uintptr_t)t.grad & ga) || (((uintptr_t)t.m | (uintptr_t)t.v) & sa) ||
+        (((uintptr_t)t.master | (uintptr_t)t.m_scale | (uintptr_t)t.v_scale) & 3))
+      return fail(FEF_ERR_INVALID_ARG, "tensor %d: addresses must be aligned to their elements", i);
+    const size_t n = (size_t)t.n, s = eight ? 1 : 4, blocks = (n + fef::kAdamwBlock - 1) / fef::kAdamwBlock * 4;
+    add(t.param, n * (pa + 1), true);
+    add(t.grad, n * (ga + 1), false);
+    if (t.master) add(t.master, n * 4, true);
+    add(t.m, n * s, true);
+    add(t.v, n * s, true);
+    if (eight) {
+      add(t.m_scale, blocks, true);
+      add(t.v_scale, blocks, true);
+    }
+  }
+  std::sort(ranges.get(), ranges.get() + used, [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  uintptr_t any = 0, written = 0;  // ends of the ranges so far
+  for (size_t i = 0; i < used; ++i) {
+    const Range& r = ranges[i];
+    if (r.begin < (r.written ? any : written)) return fail(FEF_ERR_INVALID_ARG, "tensors of the step overlap");
+    any = std::max(any, r.end);
+    if (r.written) written = std::max(written, r.end);
+  }
+  return FEF_OK;
+}
+}  // namespace
+
+fef_status fef_adamw_step(const fef_adamw_params* prm, const fef_adamw_tensor* tensors, int32_t count) {
+  const fef_status s = check_adamw(prm, tensors, count);
+  if (s != FEF_OK) return s;
+  fef::AdamwConst c{};
+  c.lr = (float)prm->lr;
+  c.b1 = (float)prm->beta1; c.one_b1 = (float)(1.0 - prm->beta1);
+  c.b2 = (float)prm->beta2; c.one_b2 = (float)(1.0 - prm->beta2);
+  c.c1 = (float)(1.0 / (1.0 - std::pow(prm->beta1, (double)prm->step)));
+  c.c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(prm->beta2, (double)prm->step)));
+  c.eps = (float)prm->eps;
+  c.schedule = prm->schedule; c.grad_scale = prm->grad_scale;
+  const bool eight = prm->state_dtype == FEF_STATE_E4M3;
+  fef::AdamwTensor some[fef::kAdamwTensors];  // a launch's worth at a time
+  for (int32_t i = 0; i < count;) {
+    int k = 0;
+    for (; i < count && k < fef::kAdamwTensors; ++i) {
+      const fef_adamw_tensor& t = tensors[i];
+      if (t.n == 0) continue;
+      const uintptr_t all = (uintptr_t)t.param | (uintptr_t)t.grad | (uintptr_t)t.master | (eight ? 0 : (uintptr_t)t.m | (uintptr_t)t.v);
+      const uintptr_t codes = eight ? (uintptr_t)t.m | (uintptr_t)t.v : 0;
+      some[k++] = fef::AdamwTensor{t.param, t.grad, t.master, t.m, t.v, t.m_scale, t.v_scale, (long)t.n, (float)t.weight_decay,
+                                   !(all & 15) && !(codes & 3)};
+    }
+    const hipError_t e = fef::launch_adamw(c, some, k, prm->dtype == FEF_BF16, prm->grad_dtype == FEF_BF16, eight, (hipStream_t)prm->stream);
+    if (e != hipSuccess) return fail(FEF_ERR_HIP, "AdamW kernel launch: %s", hipGetErrorString(e));
+  }
   return FEF_OK;
 }
 

@@ -196,4 +196,27 @@ struct EditArgs {
 int edit_partials(int V);  // (max, sum exp) pairs per row
 hipError_t launch_edit(const EditArgs& a);
 
+// The AdamW step: what is the same for all tensors, and a tensor.
+constexpr int kAdamwBlock = 256;             // elements under one scale of an 8-bit state
+constexpr float kAdamwLeast = 0x1p-100f;     // a block of smaller magnitudes is held as zeros
+constexpr int kAdamwChunk = 4096;            // elements per workgroup
+constexpr int kAdamwTensors = 48;            // tensors per launch: what fits the kernel's arguments
+constexpr long kAdamwGroups = (1L << 24) - 1;  // workgroups per launch: 2^32 threads
+struct AdamwConst {
+  float lr, c1, c2, b1, one_b1, b2, one_b2, eps;  // c1 = 1 / (1 - b1^t), c2 = 1 / sqrt(1 - b2^t)
+  const float* schedule;    // [3] lr, c1, c2 on the device, or NULL
+  const float* grad_scale;  // or NULL
+};
+struct AdamwTensor {
+  void* param;
+  const void* grad;
+  float* master;  // or NULL
+  void *m, *v;
+  float *m_scale, *v_scale;
+  long n;
+  float weight_decay;
+  int wide;  // all addresses suit vector loads
+};
+hipError_t launch_adamw(const AdamwConst& c, const AdamwTensor* tensors, int count, bool bf16, bool grad_bf16, bool eight, hipStream_t stream);
+
 }  // namespace fef
