@@ -341,6 +341,52 @@ size_t fef_verify_logits_workspace_bytes(const fef_params* prm, int32_t K, int32
 fef_status fef_verify_logits(const fef_params* prm, const float* logits, int64_t ld, int32_t K, int32_t block, uint64_t seed,
                              int32_t* out_tokens, int32_t* out_accept_len, uint8_t* out_remask);
 
+/* Truncated laws and draws from them: top-k, top-p and min-p over the logits of each slot, and a token by a given uniform.  With y a
+ * slot's logits times 1 / tau in float32, a token exists if y is a number of -2e38 or more, and the tokens are ordered by y descending,
+ * equal ones by id ascending.  With w = exp(y - max y), what is kept is the shortest of these beginnings of that order:
+ *   the first top_k tokens
+ *   the fewest tokens whose mass sum w reaches top_p times the mass of what top_k leaves
+ *   the tokens with w >= min_p (that is, a probability of min_p times the largest one or more)
+ * and the first token always.  A limit that is NaN, top_k <= 0, top_p >= 1 and min_p <= 0 limit nothing.  The token drawn is
+ * min{v kept : sum of w over the kept tokens up to v, in the order of the ids, >= u times the mass kept}, as everywhere in this library.
+ * Masses are sums of whole numbers of 2^-s, in top_p relative to weights of neighbouring tokens (within exp(1/32), or as small as a
+ * type of 64 bits allows), s = 61 - the bits of V: results do not depend on the order of the additions.  A token whose weight is below
+ * 2^-(s+1) may be kept, but is not drawn.
+ * A slot without tokens, one with a +inf or a NaN, and one whose temperature is negative or NaN has no law: nothing is kept, its token
+ * is -1, its confidence 0, its log-sum-exp -inf, its truncated logits are -inf throughout.
+ * The truncated logits can be a half of a round (fef_verify_logits), which then draws from the truncated laws. */
+typedef struct {
+  uint32_t struct_size;        /* = sizeof(fef_draw_params)                                          */
+  int32_t B, K, V;             /* sequences, window slots (<= FEF_MAX_K), vocabulary (<= 2^29)       */
+  int32_t dtype;               /* fef_dtype of the logits                                            */
+  float temperature;           /* tau > 0, 1 / tau finite                                            */
+  int64_t seq_stride;          /* elements from a sequence's logits to the next one's, >= 0          */
+  int64_t slot_stride;         /* elements from a slot's logits to the next one's, >= 0              */
+  int64_t out_seq_stride;      /* the same of the truncated logits; their rows must not overlap      */
+  int64_t out_slot_stride;
+  const float* temperatures;   /* [B] in place of temperature, or NULL; 0 (and what has no finite reciprocal) keeps the first token of the
+                                  order alone, with y the logits themselves                            */
+  const int32_t* top_k;        /* [B] each, NULL: no limit                                           */
+  const float* top_p;
+  const float* min_p;
+  const float* uniforms;       /* [B, K] u, clamped to [0, 1]; NULL: 0                               */
+  float* out_lse;              /* [B, K] log-sum-exp of the truncated logits; outputs may be NULL    */
+  int32_t* out_kept;           /* [B, K] tokens kept                                                 */
+  int32_t* out_tokens;         /* [B, K]                                                             */
+  float* out_conf;             /* [B, K] the token's probability in the truncated law                */
+  void* workspace;             /* device scratch, 256-byte aligned                                   */
+  size_t workspace_bytes;
+  void* stream;                /* hipStream_t; NULL = the null stream                                */
+} fef_draw_params;
+
+/* Bytes of device workspace fef_draw_logits needs (depends on B, K, V alone); 0 if the arguments are invalid. */
+size_t fef_draw_workspace_bytes(const fef_draw_params* prm);
+
+/*   logits  [B, K, V] device, strides above, aligned to its elements
+ *   out     [B, K, V] device float, strides above: y of the tokens kept, -inf elsewhere; NULL: not wanted.  Must not overlap `logits`
+ * Conventions and error behaviour as in fef_verify_step. */
+fef_status fef_draw_logits(const fef_draw_params* prm, const void* logits, float* out);
+
 /* One AdamW step over a list of tensors (the step of Algorithm 1 after the gradients).  For every element, with g its gradient times
  * *grad_scale, and p its float32 copy `master` where there is one, else the parameter:
  *   m <- beta1 m + (1 - beta1) g

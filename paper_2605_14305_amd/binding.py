@@ -29,7 +29,8 @@ EXPORTS = ["fef_workspace_bytes", "fef_verify_step", "fef_select_gemm", "fef_uni
            "fef_status_string", "fef_last_error", "fef_abi_version", "fef_copy_probe", "fef_read_probe",
            "fef_cross_entropy_workspace_bytes", "fef_head_cross_entropy", "fef_topn_step",
            "fef_verify_step_static", "fef_mx4_logits", "fef_edit_workspace_bytes", "fef_edit_logits",
-           "fef_verify_logits_workspace_bytes", "fef_verify_logits", "fef_adamw_step"]
+           "fef_verify_logits_workspace_bytes", "fef_verify_logits", "fef_adamw_step",
+           "fef_draw_workspace_bytes", "fef_draw_logits"]
 FEF_STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -81,6 +82,26 @@ class fef_edit_params(ctypes.Structure):
 
 _EDIT_PARAMS_SIZE = ctypes.sizeof(fef_edit_params)
 _PACK_EDIT = struct.Struct("@I4if4qi7Pi2PiPPNP").pack_into  # fef_edit_params, field by field in native alignment
+
+
+class fef_draw_params(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("B", ctypes.c_int32), ("K", ctypes.c_int32), ("V", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("temperature", ctypes.c_float),
+        ("seq_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64),
+        ("out_seq_stride", ctypes.c_int64), ("out_slot_stride", ctypes.c_int64),
+        ("temperatures", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p),
+        ("uniforms", ctypes.c_void_p),
+        ("out_lse", ctypes.c_void_p), ("out_kept", ctypes.c_void_p), ("out_tokens", ctypes.c_void_p), ("out_conf", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+_DRAW_PARAMS_SIZE = ctypes.sizeof(fef_draw_params)
+_PACK_DRAW = struct.Struct("@I4if4q10PNP").pack_into  # fef_draw_params, field by field in native alignment
 
 
 class fef_adamw_tensor(ctypes.Structure):
@@ -164,6 +185,10 @@ def lib():
         L.fef_edit_workspace_bytes.argtypes = [ctypes.POINTER(fef_edit_params)]
         L.fef_edit_logits.restype = ctypes.c_int
         L.fef_edit_logits.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+        L.fef_draw_workspace_bytes.restype = ctypes.c_size_t
+        L.fef_draw_workspace_bytes.argtypes = [ctypes.POINTER(fef_draw_params)]
+        L.fef_draw_logits.restype = ctypes.c_int
+        L.fef_draw_logits.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
         L.fef_adamw_step.restype = ctypes.c_int
         L.fef_adamw_step.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32]
         if L.fef_abi_version() != ABI_VERSION:
@@ -524,6 +549,53 @@ class EditLogits:
         if r != FEF_OK:
             raise FefError(r, fef_last_error())
         return out, self.out_lse
+
+
+class DrawLogits:
+    """Truncation of the laws of logits [B, K, V] of `dtype` ("f32" or "bf16", any strides whose last is 1), and a token of each
+    (fef_draw_logits).  Holds workspace and outputs of one shape; a call returns tokens [B, K] (int32), their probabilities, how many tokens
+    are kept (int32), log-sum-exps, and the truncated logits (float32 [B, K, V], or None with write=False), or `out` if the caller gives
+    one, which may not be the logits.  uniforms [B, K]: float32; without them a token is the smallest kept one.  Limits of each sequence,
+    all optional: top_k [B] (int32), top_p, min_p [B] (float32); temperatures [B] (float32) stand in for `temperature`, 0 for the first
+    token alone."""
+
+    def __init__(self, B, K, V, dtype="f32", device="cuda", write=True):
+        self.B, self.K, self.V, self.device = B, K, V, torch.device(device)
+        self.dtype = FEF_BF16 if dtype == "bf16" else FEF_F32
+        self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        p = fef_draw_params(struct_size=_DRAW_PARAMS_SIZE, B=B, K=K, V=V, dtype=self.dtype, temperature=1.0)
+        n = lib().fef_draw_workspace_bytes(ctypes.byref(p))
+        if n == 0:
+            raise FefError(FEF_ERR_INVALID_ARG, fef_last_error())
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self.out = torch.empty(B, K, V, dtype=torch.float32, device=self.device) if write else None
+        self.out_lse, self.out_conf = (torch.empty(B, K, dtype=torch.float32, device=self.device) for _ in range(2))
+        self.out_tokens, self.out_kept = (torch.empty(B, K, dtype=torch.int32, device=self.device) for _ in range(2))
+        self._params = ctypes.create_string_buffer(_DRAW_PARAMS_SIZE)
+        self._outputs = [t.data_ptr() for t in (self.out_lse, self.out_kept, self.out_tokens, self.out_conf, self.workspace)]
+
+    def __call__(self, logits, uniforms=None, temperature=1.0, top_k=None, top_p=None, min_p=None, temperatures=None, out=None):
+        B, K, V = shape = (self.B, self.K, self.V)
+        if out is None:
+            out = self.out
+        assert logits.shape == shape and logits.dtype == self.torch_dtype and logits.is_cuda
+        s = logits.stride()
+        assert V == 1 or s[2] == 1
+        o = (0, 0)
+        if out is not None:
+            assert out.shape == shape and out.dtype == torch.float32 and out.is_cuda and (V == 1 or out.stride(2) == 1)
+            o = out.stride()
+        lists = []
+        for t, dtype, size in ((temperatures, torch.float32, (B,)), (top_k, torch.int32, (B,)), (top_p, torch.float32, (B,)),
+                               (min_p, torch.float32, (B,)), (uniforms, torch.float32, (B, K))):
+            assert t is None or (t.dtype == dtype and t.shape == size and t.is_contiguous() and t.is_cuda)
+            lists.append(0 if t is None else t.data_ptr())
+        _PACK_DRAW(self._params, 0, _DRAW_PARAMS_SIZE, B, K, V, self.dtype, temperature, s[0], s[1], o[0], o[1], *lists, *self._outputs,
+                   self.workspace.numel(), _stream(self.device))
+        r = (_lib or lib()).fef_draw_logits(self._params, logits.data_ptr(), _ptr(out))
+        if r != FEF_OK:
+            raise FefError(r, fef_last_error())
+        return self.out_tokens, self.out_conf, self.out_kept, self.out_lse, out
 
 
 class VerifyLogits:

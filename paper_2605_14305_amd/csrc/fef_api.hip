@@ -610,6 +610,11 @@ fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* c
 }
 
 namespace {
+// Rows of an output one behind another, slots inside sequences or sequences inside slots.
+bool rows_apart(int B, int K, int V, int64_t sq, int64_t sl) {
+  return (K == 1 || sl >= V) && (B == 1 || sq >= V) && (K == 1 || B == 1 || sq >= sl * (K - 1) + V || sl >= sq * (B - 1) + V);
+}
+
 fef_status check_edit(const fef_edit_params* p, size_t* total) {
   if (!p) return fail(FEF_ERR_INVALID_ARG, "params is NULL");
   if (p->struct_size != sizeof(fef_edit_params))
@@ -627,11 +632,7 @@ fef_status check_edit(const fef_edit_params* p, size_t* total) {
     return fail(FEF_ERR_INVALID_ARG, "masks must be 0, 1 or K (got %d)", p->masks);
   for (const int64_t s : {p->seq_stride, p->slot_stride, p->out_seq_stride, p->out_slot_stride})
     if (s < 0 || s > (1L << 40)) return fail(FEF_ERR_INVALID_ARG, "strides must lie in [0, 2^40]");
-  // rows of the output one behind another, slots inside sequences or sequences inside slots
-  const int64_t sq = p->out_seq_stride, sl = p->out_slot_stride;
-  const bool apart = (p->K == 1 || sl >= p->V) && (p->B == 1 || sq >= p->V) &&
-                     (p->K == 1 || p->B == 1 || sq >= sl * (p->K - 1) + p->V || sl >= sq * (p->B - 1) + p->V);
-  if (!apart) return fail(FEF_ERR_INVALID_ARG, "rows of the output overlap");
+  if (!rows_apart(p->B, p->K, p->V, p->out_seq_stride, p->out_slot_stride)) return fail(FEF_ERR_INVALID_ARG, "rows of the output overlap");
   *total = align_up((size_t)p->B * p->K * (size_t)fef::edit_partials(p->V) * sizeof(float2), 256);
   return FEF_OK;
 }
@@ -678,6 +679,59 @@ fef_status fef_edit_logits(const fef_edit_params* p, const void* logits, float* 
   a.stream = (hipStream_t)p->stream;
   const hipError_t e = fef::launch_edit(a);
   if (e != hipSuccess) return fail(FEF_ERR_HIP, "edit kernel launch: %s", hipGetErrorString(e));
+  return FEF_OK;
+}
+
+namespace {
+fef_status check_draw(const fef_draw_params* p, size_t* total) {
+  if (!p) return fail(FEF_ERR_INVALID_ARG, "params is NULL");
+  if (p->struct_size != sizeof(fef_draw_params))
+    return fail(FEF_ERR_INVALID_ARG, "struct_size %u does not match this library's %zu", p->struct_size, sizeof(fef_draw_params));
+  if (p->B < 1 || p->V < 1) return fail(FEF_ERR_INVALID_ARG, "B and V must be >= 1 (got %d, %d)", p->B, p->V);
+  if (p->V > kMaxGivenV) return fail(FEF_ERR_INVALID_ARG, "V = %d exceeds 2^29", p->V);
+  if (p->K < 1 || p->K > FEF_MAX_K) return fail(FEF_ERR_INVALID_ARG, "K = %d out of range [1, %d]", p->K, FEF_MAX_K);
+  // (a workgroup of 1024 threads per row, and less than 2^32 threads)
+  if ((long)p->B * p->K > (1L << 21)) return fail(FEF_ERR_INVALID_ARG, "B*K = %ld exceeds 2^21 rows per call", (long)p->B * p->K);
+  if (p->dtype != FEF_BF16 && p->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
+  if (!scales_logits(p->temperature)) return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number with a finite reciprocal");
+  for (const int64_t s : {p->seq_stride, p->slot_stride, p->out_seq_stride, p->out_slot_stride})
+    if (s < 0 || s > (1L << 40)) return fail(FEF_ERR_INVALID_ARG, "strides must lie in [0, 2^40]");
+  *total = align_up(fef::draw_workspace(p->B * p->K, p->V), 256);
+  return FEF_OK;
+}
+}  // namespace
+
+size_t fef_draw_workspace_bytes(const fef_draw_params* prm) {
+  size_t total;
+  return check_draw(prm, &total) == FEF_OK ? total : 0;
+}
+
+fef_status fef_draw_logits(const fef_draw_params* p, const void* logits, float* out) {
+  size_t total;
+  const fef_status s = check_draw(p, &total);
+  if (s != FEF_OK) return s;
+  if (!logits) return fail(FEF_ERR_INVALID_ARG, "logits must not be NULL");
+  if ((uintptr_t)logits & (p->dtype == FEF_BF16 ? 1 : 3) || (uintptr_t)out & 3)
+    return fail(FEF_ERR_INVALID_ARG, "logits and out must be aligned to their elements");
+  if ((const void*)out == logits) return fail(FEF_ERR_INVALID_ARG, "out must not be the logits: a row is read several times");
+  if (out && !rows_apart(p->B, p->K, p->V, p->out_seq_stride, p->out_slot_stride)) return fail(FEF_ERR_INVALID_ARG, "rows of the output overlap");
+  const uintptr_t lists = (uintptr_t)p->temperatures | (uintptr_t)p->top_k | (uintptr_t)p->top_p | (uintptr_t)p->min_p | (uintptr_t)p->uniforms |
+                          (uintptr_t)p->out_lse | (uintptr_t)p->out_kept | (uintptr_t)p->out_tokens | (uintptr_t)p->out_conf;
+  if (lists & 3) return fail(FEF_ERR_INVALID_ARG, "limits, uniforms and outputs must be 4-byte aligned");
+  if (!p->workspace) return fail(FEF_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", total);
+  if ((uintptr_t)p->workspace & 255) return fail(FEF_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (p->workspace_bytes < total) return fail(FEF_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", p->workspace_bytes, total);
+  fef::DrawArgs a{};
+  a.B = p->B; a.K = p->K; a.V = p->V; a.bf16 = p->dtype == FEF_BF16;
+  a.inv_tau = 1.0f / p->temperature;
+  a.logits = logits; a.seq_stride = p->seq_stride; a.slot_stride = p->slot_stride;
+  a.temperatures = p->temperatures; a.top_k = p->top_k; a.top_p = p->top_p; a.min_p = p->min_p; a.uniforms = p->uniforms;
+  a.out = out; a.out_seq_stride = p->out_seq_stride; a.out_slot_stride = p->out_slot_stride;
+  a.out_lse = p->out_lse; a.out_kept = p->out_kept; a.out_tokens = p->out_tokens; a.out_conf = p->out_conf;
+  a.workspace = p->workspace;
+  a.stream = (hipStream_t)p->stream;
+  const hipError_t e = fef::launch_draw(a);
+  if (e != hipSuccess) return fail(FEF_ERR_HIP, "draw kernel launch: %s", hipGetErrorString(e));
   return FEF_OK;
 }
 

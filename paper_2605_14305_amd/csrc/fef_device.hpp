@@ -219,4 +219,26 @@ struct AdamwTensor {
 };
 hipError_t launch_adamw(const AdamwConst& c, const AdamwTensor* tensors, int count, bool bf16, bool grad_bf16, bool eight, hipStream_t stream);
 
+// Truncated laws and draws (fef_draw_params of the C ABI), one row per (sequence, slot).
+struct DrawArgs {
+  int B, K, V, bf16;
+  float inv_tau;
+  const void* logits;
+  long seq_stride, slot_stride;
+  const float* temperatures;  // [B], any of these NULL: none
+  const int32_t* top_k;
+  const float *top_p, *min_p;
+  const float* uniforms;  // [B*K]
+  float* out;
+  long out_seq_stride, out_slot_stride;
+  float* out_lse;  // [B*K], any of these NULL: not wanted
+  int32_t* out_kept;
+  int32_t* out_tokens;
+  float* out_conf;
+  void* workspace;
+  hipStream_t stream;
+};
+size_t draw_workspace(int rows, int V);
+hipError_t launch_draw(const DrawArgs& a);
+
 }  // namespace fef
