@@ -262,6 +262,26 @@ size_t fef_cross_entropy_workspace_bytes(const fef_params* prm, int32_t R);
 fef_status fef_head_cross_entropy(const fef_params* prm, const void* h, const void* W_vocab,
                                   const int32_t* labels, int32_t R, float* out_ce, float* out_loss);
 
+/* The same loss with its gradients: of sum_m w_m CE_m (w_m = weights[m], what the program's own loss passes back to row m; 1 without
+ * weights) in h and in W_vocab,
+ *   G[m, v] = w_m (p_theta(v) - [v = label_m]) / tau,   grad_h = G W,   grad_w = G^T h
+ *   h, W_vocab, labels, out_ce, out_loss   as in fef_head_cross_entropy (out_loss: the sum of out_ce, without weights)
+ *   weights  [R]    device float, or NULL
+ *   grad_h   [R, d] device, dtype prm->dtype, 16-byte aligned; NULL: not wanted
+ *   grad_w   [V, d] device, dtype prm->dtype, 16-byte aligned; NULL: not wanted, but not both
+ * The gradients are written whole, whatever was there.  A row whose label is negative has no part in any of it: its CE and its row of
+ * grad_h are 0, and h is not looked at there for grad_w.  A label >= V makes the row's CE and grad_h NaN, and grad_w with them.
+ * bf16: the logits are float32, G is rounded to bf16 (half a step of 2^-8 of each element) as an operand of the matrix cores, sums are held in
+ * 32 bits, grad_h and grad_w are rounded once.  f32: float32 throughout.  Rows are taken 8192 at a time; the order of all sums
+ * depends on the sizes alone.
+ * Fields of prm that are read: struct_size, d, V (at most 2^29), dtype, temperature (1 / tau finite), gemm_variant (AUTO, or what AUTO takes: TILED256 or
+ * F32), workspace, workspace_bytes (at least fef_cross_entropy_grad_workspace_bytes, which depends on R, d, V and dtype alone; 0 if the
+ * arguments are invalid), stream.  ev_head_begin and ev_head_end must be NULL.  bf16: d a positive multiple of 64.  1 <= R <= 2^24.
+ * Conventions and error behaviour as in fef_verify_step. */
+size_t fef_cross_entropy_grad_workspace_bytes(const fef_params* prm, int32_t R);
+fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, const void* W_vocab, const int32_t* labels,
+                                       const float* weights, int32_t R, float* out_ce, float* out_loss, void* grad_h, void* grad_w);
+
 /* Logits of the vocabulary head from a copy of W in 4 bits (the OCP MX form, MXFP4):
  *   out_logits[r, v] = (1 / tau) sum_k h[r, k] w[v, k],   w[v, k] = e2m1(code[v, k]) 2^(scale[v, k / 32] - 127)
  * The draft half of a round may read such a copy instead of W (17/64 of the bytes): a round stays exact whatever law its

@@ -30,7 +30,7 @@ EXPORTS = ["fef_workspace_bytes", "fef_verify_step", "fef_select_gemm", "fef_uni
            "fef_cross_entropy_workspace_bytes", "fef_head_cross_entropy", "fef_topn_step",
            "fef_verify_step_static", "fef_mx4_logits", "fef_edit_workspace_bytes", "fef_edit_logits",
            "fef_verify_logits_workspace_bytes", "fef_verify_logits", "fef_adamw_step",
-           "fef_draw_workspace_bytes", "fef_draw_logits"]
+           "fef_draw_workspace_bytes", "fef_draw_logits", "fef_cross_entropy_grad_workspace_bytes", "fef_head_cross_entropy_grad"]
 FEF_STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -185,6 +185,11 @@ def lib():
         L.fef_edit_workspace_bytes.argtypes = [ctypes.POINTER(fef_edit_params)]
         L.fef_edit_logits.restype = ctypes.c_int
         L.fef_edit_logits.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+        L.fef_cross_entropy_grad_workspace_bytes.restype = ctypes.c_size_t
+        L.fef_cross_entropy_grad_workspace_bytes.argtypes = [ctypes.POINTER(fef_params), ctypes.c_int32]
+        L.fef_head_cross_entropy_grad.restype = ctypes.c_int
+        L.fef_head_cross_entropy_grad.argtypes = [ctypes.POINTER(fef_params), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                                  ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
         L.fef_draw_workspace_bytes.restype = ctypes.c_size_t
         L.fef_draw_workspace_bytes.argtypes = [ctypes.POINTER(fef_draw_params)]
         L.fef_draw_logits.restype = ctypes.c_int
@@ -314,6 +319,39 @@ class HeadCrossEntropy:
         if s != FEF_OK:
             raise FefError(s, fef_last_error())
         return self.out_ce, self.out_loss
+
+
+class HeadCrossEntropyGrad:
+    """Cross-entropy of R rows through the vocabulary head with its gradients in h and W (fef_head_cross_entropy_grad); holds workspace and
+    outputs of one shape.  A call returns out_ce [R], out_loss [1], grad_h [R, d] and grad_w [V, d] (None where the constructor was told
+    so).  `weights` [R] (float32): the gradient of the program's loss in each row's cross-entropy, 1 if left out."""
+
+    def __init__(self, R, d, V, dtype="bf16", device="cuda", grad_h=True, grad_w=True):
+        self.R, self.d, self.V, self.device = R, d, V, torch.device(device)
+        self.dtype = FEF_BF16 if dtype == "bf16" else FEF_F32
+        self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self._params = make_params(1, d, V, dtype=self.dtype)
+        n = lib().fef_cross_entropy_grad_workspace_bytes(ctypes.byref(self._params), R)
+        if n == 0:
+            raise FefError(FEF_ERR_INVALID_ARG, fef_last_error())
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self.out_ce = torch.empty(R, dtype=torch.float32, device=self.device)
+        self.out_loss = torch.empty(1, dtype=torch.float32, device=self.device)
+        self.grad_h = torch.empty(R, d, dtype=self.torch_dtype, device=self.device) if grad_h else None
+        self.grad_w = torch.empty(V, d, dtype=self.torch_dtype, device=self.device) if grad_w else None
+
+    def __call__(self, h, W_vocab, labels, weights=None, temperature=1.0):
+        for t, shape, dt in ((h, (self.R, self.d), self.torch_dtype), (W_vocab, (self.V, self.d), self.torch_dtype),
+                             (labels, (self.R,), torch.int32), (weights, (self.R,), torch.float32)):
+            assert t is None or (t.shape == shape and t.dtype == dt and t.is_contiguous() and t.is_cuda)
+        p = self._params
+        p.temperature = temperature
+        p.workspace, p.workspace_bytes, p.stream = self.workspace.data_ptr(), self.workspace.numel(), _stream(self.device)
+        s = (_lib or lib()).fef_head_cross_entropy_grad(ctypes.byref(p), h.data_ptr(), W_vocab.data_ptr(), labels.data_ptr(), _ptr(weights), self.R,
+                                                        self.out_ce.data_ptr(), self.out_loss.data_ptr(), _ptr(self.grad_h), _ptr(self.grad_w))
+        if s != FEF_OK:
+            raise FefError(s, fef_last_error())
+        return self.out_ce, self.out_loss, self.grad_h, self.grad_w
 
 
 class VerifyStep:

@@ -73,4 +73,9 @@ hipError_t launch_ce_finish(const CeArgs& a) {
   return hipGetLastError();
 }
 
+hipError_t launch_ce_sum(const CeArgs& a) {
+  hipLaunchKernelGGL(ce_sum_kernel, dim3(1), dim3(NT), 0, a.stream, a);
+  return hipGetLastError();
+}
+
 }  // namespace fef

@@ -610,6 +610,148 @@ fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* c
 }
 
 namespace {
+constexpr int kGradRows = 8192;  // rows of a block: its logits and G lie in the workspace (8.3 GB and half of that at V = 126464)
+
+struct GradLayout {
+  int rows, padded, nT, shares_h, blocks;
+  long ldl;
+  size_t off_z, off_partials, off_g, off_h, off_part, off_acc, total;
+};
+
+fef_status grad_layout(const fef_params* p, int32_t R, GradLayout* L) {
+  if (!p) return fail(FEF_ERR_INVALID_ARG, "params is NULL");
+  if (p->struct_size != sizeof(fef_params))
+    return fail(FEF_ERR_INVALID_ARG, "struct_size %u does not match this library's %zu", p->struct_size, sizeof(fef_params));
+  if (R < 1 || R > (1 << 24)) return fail(FEF_ERR_INVALID_ARG, "R = %d out of range [1, 2^24]", R);
+  if (p->V < 1 || p->d < 1) return fail(FEF_ERR_INVALID_ARG, "V and d must be positive");
+  if (p->V > kMaxGivenV) return fail(FEF_ERR_INVALID_ARG, "V = %d exceeds 2^29", p->V);
+  if (p->d > (1 << 20)) return fail(FEF_ERR_INVALID_ARG, "d = %d exceeds 2^20", p->d);
+  if (p->dtype != FEF_BF16 && p->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
+  const bool bf16 = p->dtype == FEF_BF16;
+  if (bf16 && p->d % 64 != 0) return fail(FEF_ERR_INVALID_ARG, "bf16 needs d to be a multiple of 64 (got %d)", p->d);
+  if (!scales_logits(p->temperature)) return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number with a finite reciprocal");
+  if (p->gemm_variant != FEF_GEMM_AUTO && p->gemm_variant != (bf16 ? FEF_GEMM_TILED256 : FEF_GEMM_F32))
+    return fail(FEF_ERR_UNSUPPORTED, "gradients run through the TILED256 (bf16) or the F32 head kernel");
+  if (p->ev_head_begin || p->ev_head_end) return fail(FEF_ERR_INVALID_ARG, "ev_head_begin and ev_head_end must be NULL in this call");
+  L->rows = R < kGradRows ? R : kGradRows;
+  L->blocks = (R + kGradRows - 1) / kGradRows;
+  L->padded = bf16 ? (int)align_up((size_t)L->rows, 64) : L->rows;
+  L->ldl = (long)align_up((size_t)p->V, 64);
+  L->nT = bf16 ? (p->V + fef::kTiled256Tn - 1) / fef::kTiled256Tn : (p->V + fef::kTiledTn - 1) / fef::kTiledTn;
+  const size_t e = bf16 ? 2 : 4, d = (size_t)p->d;
+  L->shares_h = bf16 ? fef::grad_h_shares(L->rows, p->d, p->V) : fef::grad_f32_shares(L->rows, p->d, p->V);
+  size_t o = 0;
+  auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
+  L->off_z = take((size_t)L->rows * L->ldl * 4);
+  L->off_partials = take((size_t)L->rows * L->nT * sizeof(float2));
+  L->off_g = bf16 ? take((size_t)L->padded * L->ldl * 2) : L->off_z;
+  L->off_h = take((size_t)L->padded * d * e);
+  // (a last block of fewer rows may take more shares of as many rows less)
+  L->off_part = take(align_up((size_t)L->rows * d, 4) * 4 * (size_t)L->shares_h);
+  L->off_acc = take(bf16 && L->blocks > 1 ? (size_t)p->V * d * 4 : 0);
+  L->total = o;
+  return FEF_OK;
+}
+}  // namespace
+
+size_t fef_cross_entropy_grad_workspace_bytes(const fef_params* prm, int32_t R) {
+  GradLayout L;
+  return grad_layout(prm, R, &L) == FEF_OK ? L.total : 0;
+}
+
+fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, const void* W_vocab, const int32_t* labels,
+                                       const float* weights, int32_t R, float* out_ce, float* out_loss, void* grad_h, void* grad_w) {
+  GradLayout L;
+  const fef_status s = grad_layout(prm, R, &L);
+  if (s != FEF_OK) return s;
+  if (!h || !W_vocab || !labels || !out_ce) return fail(FEF_ERR_INVALID_ARG, "h, W_vocab, labels and out_ce must not be NULL");
+  if (!grad_h && !grad_w) return fail(FEF_ERR_INVALID_ARG, "grad_h and grad_w must not both be NULL");
+  if (((uintptr_t)h | (uintptr_t)W_vocab | (uintptr_t)grad_h | (uintptr_t)grad_w) & 15)
+    return fail(FEF_ERR_INVALID_ARG, "h, W_vocab, grad_h and grad_w must be 16-byte aligned");
+  if (((uintptr_t)labels | (uintptr_t)weights | (uintptr_t)out_ce | (uintptr_t)out_loss) & 3)
+    return fail(FEF_ERR_INVALID_ARG, "labels, weights, out_ce and out_loss must be 4-byte aligned");
+  const bool bf16 = prm->dtype == FEF_BF16;
+  const size_t e = bf16 ? 2 : 4, d = (size_t)prm->d, V = (size_t)prm->V;
+  const struct { uintptr_t at; size_t bytes; } in[2] = {{(uintptr_t)h, R * d * e}, {(uintptr_t)W_vocab, V * d * e}},
+                                                out[2] = {{(uintptr_t)grad_h, grad_h ? R * d * e : 0}, {(uintptr_t)grad_w, grad_w ? V * d * e : 0}};
+  auto meet = [](auto& x, auto& y) { return x.bytes && y.bytes && x.at < y.at + y.bytes && y.at < x.at + x.bytes; };
+  if (meet(out[0], in[0]) || meet(out[0], in[1]) || meet(out[1], in[0]) || meet(out[1], in[1]) || meet(out[0], out[1]))
+    return fail(FEF_ERR_INVALID_ARG, "grad_h and grad_w must overlap neither each other nor h and W_vocab");
+  if (!prm->workspace) return fail(FEF_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", L.total);
+  if ((uintptr_t)prm->workspace & 255) return fail(FEF_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (prm->workspace_bytes < L.total) return fail(FEF_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", prm->workspace_bytes, L.total);
+
+  char* ws = (char*)prm->workspace;
+  hipStream_t stream = (hipStream_t)prm->stream;
+  float* const part = (float*)(ws + L.off_part);
+  float* const acc = (float*)(ws + L.off_acc);
+  hipError_t err = hipSuccess;
+  for (int b = 0; b < L.blocks; ++b) {
+    const size_t r0 = (size_t)b * kGradRows;
+    const int rows = (int)std::min((size_t)kGradRows, (size_t)R - r0);
+    const char* hb = (const char*)h + r0 * d * e;
+    fef::HeadArgs a{};
+    a.h_draft = a.h_target = hb; a.W = W_vocab;
+    a.BK = rows; a.d = prm->d; a.V = prm->V; a.row0 = 0; a.nrows = rows;
+    a.inv_tau = 1.0f / prm->temperature;
+    a.logits = (float*)(ws + L.off_z); a.ldl = L.ldl;
+    a.partials = (float2*)(ws + L.off_partials); a.nT = L.nT;
+    a.stream = stream;
+    err = bf16 ? fef::launch_head_tiled256(a) : fef::launch_head_f32(a);
+    if (err != hipSuccess) return fail(FEF_ERR_HIP, "head kernel launch: %s", hipGetErrorString(err));
+    fef::GradArgs g{};
+    g.rows = rows; g.padded = bf16 ? (int)align_up((size_t)rows, 64) : rows; g.V = prm->V; g.d = prm->d; g.nT = L.nT; g.ldl = L.ldl;
+    g.z = a.logits; g.partials = a.partials; g.labels = labels + r0; g.weights = weights ? weights + r0 : nullptr; g.inv_tau = a.inv_tau;
+    g.h = hb; g.H = grad_w ? ws + L.off_h : nullptr; g.G = ws + L.off_g; g.out_ce = out_ce + r0;
+    err = fef::launch_grad_rows(g, bf16, stream);
+    if (err != hipSuccess) return fail(FEF_ERR_HIP, "gradient kernel launch: %s", hipGetErrorString(err));
+    const size_t n_h = (size_t)rows * d, stride_h = align_up(n_h, 4), n_w = V * d;
+    char* const gh = (char*)grad_h + r0 * d * e;
+    if (bf16) {
+      if (grad_h) {
+        fef::ProductArgs p{};
+        p.A = (const __bf16*)g.G; p.lda = L.ldl; p.B = (const __bf16*)W_vocab; p.ldb = prm->d; p.b_rows = prm->V;
+        p.M = rows; p.N = prm->d; p.K = (int)L.ldl; p.shares = std::min(fef::grad_h_shares(rows, prm->d, prm->V), L.shares_h); p.stride = stride_h;
+        p.C = p.shares > 1 ? (void*)part : (void*)gh;
+        err = fef::launch_grad_h(p, stream);
+        if (err == hipSuccess && p.shares > 1) err = fef::launch_grad_sum(part, p.shares, stride_h, n_h, gh, true, stream);
+      }
+      if (err == hipSuccess && grad_w) {
+        fef::ProductArgs p{};
+        p.A = (const __bf16*)g.G; p.lda = L.ldl; p.B = (const __bf16*)g.H; p.ldb = prm->d; p.b_rows = g.padded;
+        p.M = prm->V; p.N = prm->d; p.K = g.padded; p.shares = 1; p.n_first = 1;
+        p.C = L.blocks > 1 ? (void*)acc : grad_w; p.add = b > 0;
+        err = fef::launch_grad_w(p, L.blocks > 1, stream);
+        if (err == hipSuccess && L.blocks > 1 && b + 1 == L.blocks) err = fef::launch_grad_sum(acc, 1, 0, n_w, grad_w, true, stream);
+      }
+    } else {
+      if (grad_h) {
+        fef::ProductF32Args p{};
+        p.A = (const float*)g.G; p.lda = L.ldl; p.B = (const float*)W_vocab; p.M = rows; p.N = prm->d; p.K = prm->V;
+        p.shares = std::min(fef::grad_f32_shares(rows, prm->d, prm->V), L.shares_h); p.stride = stride_h;
+        p.C = p.shares > 1 ? part : (float*)gh;
+        err = fef::launch_grad_product_f32(p, false, stream);
+        if (err == hipSuccess && p.shares > 1) err = fef::launch_grad_sum(part, p.shares, stride_h, n_h, gh, false, stream);
+      }
+      if (err == hipSuccess && grad_w) {
+        fef::ProductF32Args p{};
+        p.A = (const float*)g.G; p.lda = L.ldl; p.B = (const float*)g.H; p.M = prm->V; p.N = prm->d; p.K = rows; p.shares = 1;
+        p.C = (float*)grad_w; p.add = b > 0;
+        err = fef::launch_grad_product_f32(p, true, stream);
+      }
+    }
+    if (err != hipSuccess) return fail(FEF_ERR_HIP, "gradient product launch: %s", hipGetErrorString(err));
+  }
+  if (out_loss) {
+    fef::CeArgs c{};
+    c.R = R; c.out_ce = out_ce; c.out_loss = out_loss; c.stream = stream;
+    err = fef::launch_ce_sum(c);
+    if (err != hipSuccess) return fail(FEF_ERR_HIP, "cross-entropy kernel launch: %s", hipGetErrorString(err));
+  }
+  return FEF_OK;
+}
+
+namespace {
 // Rows of an output one behind another, slots inside sequences or sequences inside slots.
 bool rows_apart(int B, int K, int V, int64_t sq, int64_t sl) {
   return (K == 1 || sl >= V) && (B == 1 || sq >= V) && (K == 1 || B == 1 || sq >= sl * (K - 1) + V || sl >= sq * (B - 1) + V);

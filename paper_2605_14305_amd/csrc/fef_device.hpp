@@ -159,6 +159,7 @@ struct CeArgs {
   hipStream_t stream;
 };
 hipError_t launch_ce_finish(const CeArgs& a);
+hipError_t launch_ce_sum(const CeArgs& a);  // out_loss from out_ce
 
 // Logits from a head in 4 bits (MXFP4): codes [V, d / 2], scales [V, d / 32].
 struct Mx4Args {
@@ -240,5 +241,50 @@ struct DrawArgs {
 };
 size_t draw_workspace(int rows, int V);
 hipError_t launch_draw(const DrawArgs& a);
+
+// Gradients of the head's cross-entropy.  G from z: rows [0, rows) of a block of rows, filled up with zero rows to `padded`.
+struct GradArgs {
+  int rows, padded, V, d, nT;
+  long ldl;                // of z and G, a multiple of 64
+  const float* z;          // [rows, ldl] logits
+  const float2* partials;  // [rows, nT]
+  const int32_t* labels;   // [rows]
+  const float* weights;    // [rows] or NULL
+  float inv_tau;
+  const void* h;           // [rows, d]
+  void* H;                 // [padded, d] h with zeros in rows that do not count; NULL: not wanted
+  void* G;                 // [padded, ldl], the type of h; may be z
+  float* out_ce;           // [rows]
+};
+// C[m, n] = sum_k A[m, k] B[k, n], bf16; shares > 1, or partial: float sums [shares][stride], else C is bf16
+struct ProductArgs {
+  const __bf16* A;
+  long lda;
+  const __bf16* B;  // [b_rows, ldb]
+  long ldb;
+  int b_rows, M, N, K;  // K, N multiples of 64
+  void* C;
+  int shares;
+  size_t stride;
+  int add;      // partial: onto what is there
+  int n_first;  // neighbouring workgroups take neighbouring columns (else rows)
+};
+struct ProductF32Args {
+  const float* A;
+  long lda;
+  const float* B;  // [K, N]
+  int M, N, K;
+  float* C;
+  int shares;
+  size_t stride;
+  int add;
+};
+hipError_t launch_grad_rows(const GradArgs& a, bool bf16, hipStream_t stream);
+int grad_h_shares(int rows, int d, int V);
+hipError_t launch_grad_h(const ProductArgs& a, hipStream_t stream);
+hipError_t launch_grad_w(const ProductArgs& a, bool partial, hipStream_t stream);
+hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t n, void* out, bool bf16, hipStream_t stream);
+int grad_f32_shares(int M, int N, int K);
+hipError_t launch_grad_product_f32(const ProductF32Args& a, bool at, hipStream_t stream);
 
 }  // namespace fef

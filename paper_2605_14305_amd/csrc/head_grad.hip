@@ -1,0 +1,339 @@
+// Gradients of the head's cross-entropy (fef_head_cross_entropy_grad), bf16: with z = H W^T / tau, and G[r, v] =
+// g_r (exp(z[r, v] - lse_r) - [v = label_r]) / tau, grad_H = G W and grad_W = G^T H.
+//
+// z comes from the head kernels, G is made from it in one pass (rounded to bf16: it is an operand of the matrix cores, whose products
+// are summed in 32 bits), and two products of 2 R d V operations follow, each on the same kernel: C[m, n] = sum_k A[m, k] B[k, n].  B (W, or
+// H) has n contiguous, so its fragments are read from LDS transposed (ds_read_b64_tr_b16).  A is G, with k (the tokens, for grad_H)
+// or m (the tokens, for grad_W: read transposed too) contiguous.  No transposed copy of anything is made.
+#include <type_traits>
+
+#include "head_common.hpp"
+
+namespace fef {
+namespace {
+
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---------------------------------------------------------------------------------------------
+// G from z
+// ---------------------------------------------------------------------------------------------
+constexpr int NT = 256, kChunk = 4096;  // tokens per workgroup
+
+// Log-sum-exp of a row from its partials, in every thread; fixed order.
+__device__ __forceinline__ float row_lse(const float2* P, int n) {
+  __shared__ float2 part[NT / kWave];
+  const int tid = threadIdx.x;
+  float mx = kLowest, sm = 0.f;
+  for (int t = tid; t < n; t += NT) {
+    const float2 p = P[t];
+    const float m = fmaxf(mx, p.x);
+    sm = sm * expf(mx - m) + p.y * expf(p.x - m);
+    mx = m;
+  }
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const float mo = __shfl_xor(mx, d), so = __shfl_xor(sm, d);
+    const float m = fmaxf(mx, mo);
+    sm = sm * expf(mx - m) + so * expf(mo - m);
+    mx = m;
+  }
+  if ((tid & 63) == 0) part[tid >> 6] = make_float2(mx, sm);
+  __syncthreads();
+  mx = part[0].x;
+#pragma unroll
+  for (int w = 1; w < NT / kWave; ++w) mx = fmaxf(mx, part[w].x);
+  sm = 0.f;
+#pragma unroll
+  for (int w = 0; w < NT / kWave; ++w) sm += part[w].y * expf(part[w].x - mx);
+  return mx + logf(sm);
+}
+
+// A row of G (zeros behind the vocabulary, in rows that do not count and in the rows that fill up a block of 64), and the row's loss.
+// G may be z itself (float).
+template <class T>
+__global__ __launch_bounds__(NT) void grad_rows_kernel(GradArgs a) {
+  const int r = blockIdx.y, tid = threadIdx.x;
+  const int v0 = blockIdx.x * kChunk, v1 = min((int)a.ldl, v0 + kChunk);
+  T* G = (T*)a.G + (size_t)r * a.ldl;
+  const int label = r < a.rows ? a.labels[r] : -1;
+  if (label < 0) {  // workgroup-uniform
+    for (int v = v0 + 4 * tid; v < v1; v += 4 * NT)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) G[v + c] = (T)0.f;
+    if (blockIdx.x == 0) {
+      if (r < a.rows && tid == 0) a.out_ce[r] = 0.f;
+      if (a.H)  // (of grad_W) what such a row holds is not looked at
+        for (int k = tid; k < a.d; k += NT) ((T*)a.H)[(size_t)r * a.d + k] = (T)0.f;
+    }
+    return;
+  }
+  const float* z = a.z + (size_t)r * a.ldl;
+  const float lse = row_lse(a.partials + (size_t)r * a.nT, a.nT);
+  const bool known = label < a.V;
+  if (tid == 0 && known && label >= v0 && label < v1) a.out_ce[r] = lse - z[label];  // its own tokens only: G may be z
+  if (tid == 0 && !known && blockIdx.x == 0) a.out_ce[r] = __builtin_nanf("");
+  __syncthreads();
+  if (blockIdx.x == 0 && a.H)
+    for (int k = tid; k < a.d; k += NT) ((T*)a.H)[(size_t)r * a.d + k] = ((const T*)a.h)[(size_t)r * a.d + k];
+  const float g = (a.weights ? a.weights[r] : 1.f) * a.inv_tau;
+  for (int v = v0 + 4 * tid; v < v1; v += 4 * NT) {
+    const float4 x = *reinterpret_cast<const float4*>(z + v);
+    const float l[4] = {x.x, x.y, x.z, x.w};
+    T o[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      float p = expf(l[c] - lse);
+      if (v + c == label) p -= 1.f;
+      p *= known ? g : __builtin_nanf("");
+      o[c] = (T)(v + c < a.V ? p : 0.f);
+    }
+    if constexpr (sizeof(T) == 2) {
+      uint2 u;
+      __builtin_memcpy(&u, o, 8);
+      *reinterpret_cast<uint2*>(G + v) = u;
+    } else {
+      *reinterpret_cast<float4*>(G + v) = make_float4(o[0], o[1], o[2], o[3]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// C = A B, bf16 operands
+// ---------------------------------------------------------------------------------------------
+constexpr int kThreads = 512, BN = 256, BK = 64, WM = 2, WN = 4;
+
+// Rows of 64 k and `cols` columns in LDS, 32 bytes (16 columns) at chunk c ^ turn(k): the 32 lanes of half a transposed read, which take
+// 32 bytes of rows 8 g + {0, 1, 2, 3} of two lane groups g, fall on different banks.
+template <int COLS>
+__device__ __forceinline__ int turn(int k) {
+  if constexpr (COLS >= 128) return (k & 3) | ((k >> 3) & 1) << 2;
+  else return ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
+}
+
+// Four 16-bit values of a column of 4 rows x 16 columns whose row r lies in lanes 4 r .. 4 r + 3 of each group of 16.
+__device__ __forceinline__ bf16x4 read_turned(const char* p) {
+  typedef __attribute__((address_space(3))) shortx4* P;
+  return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(shortx4*)p));
+}
+__device__ __forceinline__ bf16x8 both(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// AT: A is [K][M] (m contiguous), else [M][K].  OUT: __bf16 for C itself, float for the partial sums of a share of k.
+template <int NR, bool AT, class OUT>
+__global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
+  constexpr int BM = 16 * NR * WM;
+  constexpr int RA = 2, RB = 3;  // stages in LDS: A one step ahead, B two
+  constexpr int kStageA = BM * BK * 2, kStageB = BN * BK * 2;
+  constexpr int kLoadsA = kStageA / 1024, LA = (kLoadsA + 7) / 8, LB = kStageB / 1024 / 8;
+  static_assert(kLoadsA >= LA && LA <= 4 && LB == 4, "");
+  constexpr int kPitch = BN + 8;  // of the tile in LDS on its way out
+  constexpr int kOut = sizeof(OUT) == 2 ? BM * kPitch * 2 : 0;
+  constexpr int kRings = RA * kStageA + RB * kStageB;
+  __shared__ __align__(16) char lds[kRings > kOut ? kRings : kOut];
+  char* const ringA = lds;
+  char* const ringB = lds + RA * kStageA;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  const int i16 = lane & 15, g = lane >> 4;
+
+  // consecutive tiles on one XCD
+  const int mt = (a.M + BM - 1) / BM, nt = (a.N + BN - 1) / BN;
+  const long tiles = (long)mt * nt * a.shares, per = (tiles + 7) / 8;
+  const long id = (long)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((long)(blockIdx.x >> 3) >= per || id >= tiles) return;
+  const int share = (int)(id / ((long)mt * nt)), at = (int)(id % ((long)mt * nt));
+  const int m0 = (a.n_first ? at / nt : at % mt) * BM, n0 = (a.n_first ? at % nt : at / mt) * BN;
+  const int nk_all = a.K / BK;
+  const int k0 = (int)((long)share * nk_all / a.shares), nk = (int)((long)(share + 1) * nk_all / a.shares) - k0;
+
+  // Direct-to-LDS loads of 1 KB: lane l fills slot (instruction, l) of 16 bytes.
+  const __bf16* ga[LA];
+  const __bf16* gb[LB];
+  const int ia0 = min(wave * LA, kLoadsA - LA);
+#pragma unroll
+  for (int q = 0; q < LA; ++q) {
+    const int s = (ia0 + q) * 64 + lane;
+    if constexpr (AT) {
+      const int k = s / (BM / 8), p = s % (BM / 8);
+      const int m = m0 + (((p >> 1) ^ turn<BM>(k)) * 16 + (p & 1) * 8);
+      ga[q] = a.A + (size_t)(k0 * BK + k) * a.lda + min(m, (a.M - 1) & ~7) - q * 512;
+    } else {
+      const int m = s / 8, c = (s & 7) ^ ((m >> 1) & 7);
+      ga[q] = a.A + (size_t)min(m0 + m, a.M - 1) * a.lda + k0 * BK + c * 8 - q * 512;
+    }
+  }
+  int b_row[LB];
+#pragma unroll
+  for (int q = 0; q < LB; ++q) {
+    const int s = (wave * LB + q) * 64 + lane;
+    const int k = s / (BN / 8), p = s % (BN / 8);
+    const int n = n0 + (((p >> 1) ^ turn<BN>(k)) * 16 + (p & 1) * 8);
+    b_row[q] = k0 * BK + k;
+    gb[q] = a.B + min(n, a.N - 8) - q * 512;
+  }
+  const uint32_t slotA = lds_offset(ringA) + ia0 * 1024, slotB = lds_offset(ringB) + wave * LB * 1024;
+  auto load_a = [&](int stage) __attribute__((always_inline)) {
+    load_group_to_lds<false>(ga, __builtin_amdgcn_readfirstlane(slotA + stage * kStageA));
+#pragma unroll
+    for (int q = 0; q < LA; ++q) ga[q] += AT ? (long)BK * a.lda : (long)BK;
+  };
+  auto load_b = [&](int stage) __attribute__((always_inline)) {
+    const __bf16* p[LB];
+#pragma unroll
+    for (int q = 0; q < LB; ++q) {
+      p[q] = gb[q] + (size_t)min(b_row[q], a.b_rows - 1) * a.ldb;  // rows past the last meet zeros of A
+      b_row[q] += BK;
+    }
+    load_group_to_lds<false>(p, __builtin_amdgcn_readfirstlane(slotB + stage * kStageB));
+  };
+
+  floatx4 acc[NR][4];
+#pragma unroll
+  for (int n = 0; n < NR; ++n)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[n][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  // byte offsets of a lane's fragments in a stage
+  const int kr = 8 * g + (i16 >> 2), cc = (i16 & 3) * 8;
+  int ob[4], oa[AT ? NR : 2];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) ob[t] = kr * (BN * 2) + ((wn * 4 + t) ^ turn<BN>(kr)) * 32 + cc;
+  if constexpr (AT) {
+#pragma unroll
+    for (int n = 0; n < NR; ++n) oa[n] = kr * (BM * 2) + ((wm * NR + n) ^ turn<BM>(kr)) * 32 + cc;
+  } else {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) oa[ks] = (wm * NR * 16 + i16) * 128 + (((ks * 4 + g) ^ ((i16 >> 1) & 7)) * 16);
+  }
+
+  if (nk > 0) {
+    load_b(0);
+    load_a(0);
+    if (nk > 1) load_b(1);
+  }
+  int sb = 0;
+  for (int k = 0; k < nk; ++k) {
+    if (k + 1 < nk) wait_newer<LB>();  // B(k + 1) may stay on its way
+    else wait_newer<0>();
+    lds_barrier();
+    if (k + 1 < nk) load_a((k + 1) & 1);
+    if (k + 2 < nk) load_b(sb == 0 ? RB - 1 : sb - 1);
+    const char* sA = ringA + (k & 1) * kStageA;
+    const char* sB = ringB + sb * kStageB;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      bf16x8 nf[4], mf[NR];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        nf[t] = both(read_turned(sB + ob[t] + ks * 32 * BN * 2), read_turned(sB + ob[t] + (ks * 32 + 4) * BN * 2));
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        if constexpr (AT) mf[n] = both(read_turned(sA + oa[n] + ks * 32 * BM * 2), read_turned(sA + oa[n] + (ks * 32 + 4) * BM * 2));
+        else mf[n] = *reinterpret_cast<const bf16x8*>(sA + oa[ks] + n * 2048);
+      }
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf[t], mf[n], acc[n][t], 0, 0, 0);
+    }
+    sb = sb == RB - 1 ? 0 : sb + 1;
+  }
+  // acc[n][t]: columns 16 t + 4 g .. + 3 of row 16 n + i16 of the wavefront's tile
+  if constexpr (sizeof(OUT) == 4) {
+    float* C = (float*)a.C + (size_t)share * a.stride;
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const int m = m0 + (wm * NR + n) * 16 + i16;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int c = n0 + (wn * 4 + t) * 16 + 4 * g;
+        if (m < a.M && c < a.N) {
+          floatx4* p = reinterpret_cast<floatx4*>(C + (size_t)m * a.N + c);
+          *p = a.add ? *p + acc[n][t] : acc[n][t];
+        }
+      }
+    }
+  } else {
+    lds_barrier();  // nobody reads the rings any more
+    __bf16* tile = reinterpret_cast<__bf16*>(lds);
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        bf16x4 o;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = (__bf16)acc[n][t][c];
+        *reinterpret_cast<bf16x4*>(tile + ((wm * NR + n) * 16 + i16) * kPitch + (wn * 4 + t) * 16 + 4 * g) = o;
+      }
+    lds_barrier();
+    __bf16* C = (__bf16*)a.C;
+    for (int s = tid; s < BM * (BN / 8); s += kThreads) {
+      const int m = s / (BN / 8), c = (s % (BN / 8)) * 8;
+      if (m0 + m < a.M && n0 + c < a.N)
+        *reinterpret_cast<bf16x8*>(C + (size_t)(m0 + m) * a.N + n0 + c) = *reinterpret_cast<const bf16x8*>(tile + m * kPitch + c);
+    }
+  }
+}
+
+// Sum of the shares' partial sums, in their order.
+template <class OUT>
+__global__ __launch_bounds__(256) void grad_sum_kernel(const float* part, int shares, size_t stride, size_t n, OUT* out) {
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  floatx4 s = *reinterpret_cast<const floatx4*>(part + i);
+  for (int j = 1; j < shares; ++j) s += *reinterpret_cast<const floatx4*>(part + (size_t)j * stride + i);
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    if (i + c < n) out[i + c] = (OUT)s[c];
+}
+
+template <int NR, bool AT>
+hipError_t launch_rows(const ProductArgs& a, bool partial, hipStream_t stream) {
+  constexpr int BM = 16 * NR * WM;
+  const long tiles = (long)((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN) * a.shares;
+  const dim3 grid((unsigned)(8 * ((tiles + 7) / 8))), threads(kThreads);
+  if (partial) hipLaunchKernelGGL((grad_product_kernel<NR, AT, float>), grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL((grad_product_kernel<NR, AT, __bf16>), grid, threads, 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_grad_rows(const GradArgs& a, bool bf16, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.ldl + kChunk - 1) / kChunk), (unsigned)a.padded), threads(NT);
+  if (bf16) hipLaunchKernelGGL(grad_rows_kernel<__bf16>, grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL(grad_rows_kernel<float>, grid, threads, 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t n, void* out, bool bf16, hipStream_t stream) {
+  const dim3 grid((unsigned)((n + 1023) / 1024)), threads(256);
+  if (bf16) hipLaunchKernelGGL(grad_sum_kernel<__bf16>, grid, threads, 0, stream, part, shares, stride, n, (__bf16*)out);
+  else hipLaunchKernelGGL(grad_sum_kernel<float>, grid, threads, 0, stream, part, shares, stride, n, (float*)out);
+  return hipGetLastError();
+}
+
+// grad_H: rows of H to a tile, and into how many shares k (the tokens) is cut so that the CUs have work.
+static int grad_h_rows(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+int grad_h_shares(int rows, int d, int V) {
+  const int bm = grad_h_rows(rows);
+  const long tiles = (long)((rows + bm - 1) / bm) * ((d + BN - 1) / BN);
+  const long steps = (V + BK - 1) / BK, want = tiles >= 256 ? 1 : 256 / tiles;
+  return (int)(want < steps ? want : steps);
+}
+
+hipError_t launch_grad_h(const ProductArgs& a, hipStream_t stream) {
+  const bool partial = a.shares > 1;
+  switch (grad_h_rows(a.M)) {
+    case 32: return launch_rows<1, false>(a, partial, stream);
+    case 64: return launch_rows<2, false>(a, partial, stream);
+    case 128: return launch_rows<4, false>(a, partial, stream);
+    default: return launch_rows<8, false>(a, partial, stream);
+  }
+}
+hipError_t launch_grad_w(const ProductArgs& a, bool partial, hipStream_t stream) { return launch_rows<8, true>(a, partial, stream); }
+
+}  // namespace fef
