@@ -2,31 +2,40 @@
 // log-sum-exp, and a token by inverse CDF.
 //
 // The order of a row's tokens is (key descending, id ascending), key being the logit's bits mapped to an unsigned number of the same order.
-// Whatever the limits, what is kept is a beginning of that order: tokens with key > T, and those with key == T up to an id I.
-//
-// One workgroup takes a row and finds (T, I) without sorting it:
-//   1. read the row: its maximum, and how many tokens and how much mass lie in each of 4096 bins of 1/32 (y - ref, ref = 0; a row whose
-//      maximum lies outside [-32, 62) is read again with ref = max - 62).  Tokens below the lowest bin are counted in it.
-//   2. sums over the bins from the top: the bin where top-k ends, and the bins where top-p can end, given what top-k may leave.
-//   3. read the row again: what lies above these bins is kept and written, what lies in them goes to a list in LDS, the rest is -inf.
+// Whatever the limits, what is kept is a beginning of that order: tokens with key > T, and those with key == T up to an id I.  (T, I) is
+// found without sorting the row:
+//   1. read the row: its maximum, and how many tokens and how much mass lie in each of 4096 bins of width 1/32, which reach from 80 below the
+//      largest of a sample of the row to 48 above it.  Tokens below all bins are counted in the lowest one; they have no mass (exp(-64) of the
+//      largest weight and less).
+//   2. sums over the topmost bins (64 below the maximum, or 32): the bin where top-k ends, and the bins where top-p can end, given what top-k may leave.
+//   3. read the row again: what lies above these bins is kept and written, what lies in them goes to a list, the rest is -inf.
 //   4. the list is sorted; rank and mass before each of its tokens give (T, I); what it keeps is written.
 //   5. the token: sums of the kept mass per tile of ids, then the ids of one tile.
-// A list longer than kList (a vocabulary of equal logits) is narrowed down by its keys instead, 12 bits per reading.
 //
 // Masses decide which token is the last, so they are exact to 2^-44 or so: a weight is computed in 64 bits and added as a whole number of
-// 2^-s, which no order of the atomics changes.  In step 1 weights are relative to their bin's middle, |y - middle| <= 1/64, where a
+// 2^-f, which no order of the atomics changes.  In step 1 weights are relative to their bin's middle, |y - middle| <= 1/64, where a
 // polynomial of degree 5 is exact to 2^-45.
+//
+// Two ways through these steps.  draw_rows_kernel: a workgroup per row, from kManyRows rows on and for short vocabularies.  Fewer long rows:
+// slices of a row, a workgroup each, in three launches: draw_bins_kernel (step 1), draw_keep_kernel (steps 2 and 3: every workgroup adds up its
+// row's bins) and draw_finish_kernel (a workgroup per row: steps 4 and 5).  What this does not serve (a list longer than kList: equal logits;
+// limits that end below step 2's bins; a maximum far above the sample) is left to left_row, which narrows down the last key by readings of
+// the row, 12 bits each.
 #include <math.h>
 
-#include "fef_device.hpp"
+#include <type_traits>
+
+#include "head_common.hpp"
+#include "wave_ops.hpp"
 
 namespace fef {
 namespace {
 
 typedef unsigned long long u64;
 
-constexpr int T = 1024, kWaves = T / kWave;
-constexpr int kBins = 4096, kList = 2048, kTiles = 512, kTile = 4 * T;
+constexpr int kBins = 4096, kList = 2048, kTiles = 512;
+constexpr int kManyRows = 128, kShort = 16384;
+constexpr int kGroupLog = 6, kGroups = 2816;  // positions of a row in groups of 64, of which step 3 reads those with a token that may be kept
 constexpr float kWidth = 32.f;  // bins per unit of y
 constexpr double kReached = 1 - 0x1p-44;  // of a mass: sums that meet top_p exactly (equal logits) are not missed for their last bits
 constexpr float kNone = -2e38f;  // smaller numbers stand for no token
@@ -40,44 +49,93 @@ __device__ __forceinline__ float of_key(unsigned k) {
 }
 
 struct Shared {
-  unsigned cnt[kBins];
-  u64 mass[kBins];       // fixed point; after the sums: the mass above the bin, a double
+  unsigned cnt[kBins];   // tokens per bin; after step 2: above the bin
+  u64 mass[kBins];       // fixed point; after step 2: the mass above the bin, a double
   u64 list[kList];
   u64 tile[kTiles];
-  u64 part[kWaves];
+  u64 part[16];
+  double power[64];      // 2^(j / 64)
   unsigned list_n, kept;
   unsigned found[4];
   double value[2];
   u64 sum;
+  unsigned above_k;      // tokens above the bin where top-k ends
+  u64 last_sum;
 };
 
-// Sum over the workgroup of everything up to and with this thread, and the total; D is u64 or double.  Fixed order.
+// t p + c, c uniform (in scalar registers: left to itself the compiler moves every constant to vector registers first)
+__device__ __forceinline__ double horner(double t, double p, double c) {
+  double r;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(t), "v"(p), "s"(c));
+  return r;
+}
+// exp(x) for x <= 1, to 2^-51 or so; each step one rounding, so that the same x gives the same bits wherever this is compiled into.
+__device__ __forceinline__ double exp64(double x, const double* power) {
+  x = fmax(x, -800.0);  // 0
+  const double k = rint(x * 92.332482616893657);  // 64 / ln 2
+  const double r = fma(k, -1.0830424696249145e-02, x), q = fma(k, -3.6219510595213e-19, r);  // ln 2 / 64 in two parts
+  const int j = (int)k;
+  const double p = horner(q, horner(q, horner(q, horner(q, horner(q, 1.0 / 120, 1.0 / 24), 1.0 / 6), 1.0 / 2), 1.0), 1.0);
+  return ldexp(power[j & 63] * p, j >> 6);
+}
+
+// Inclusive sums over the lanes of a wavefront, of u64 or double (0 is all bits clear in both).
 template <class D>
+__device__ __forceinline__ D wave_scan64(D x) {
+  auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+    const u64 b = __builtin_bit_cast(u64, x);
+    const unsigned lo = (unsigned)dpp_mov<decltype(ctrl)::value, decltype(rows)::value>(0, (int)(unsigned)b);
+    const unsigned hi = (unsigned)dpp_mov<decltype(ctrl)::value, decltype(rows)::value>(0, (int)(unsigned)(b >> 32));
+    x += __builtin_bit_cast(D, (u64)hi << 32 | lo);
+  };
+  using All = std::integral_constant<int, 0xf>;
+  step(std::integral_constant<int, kDppRowShr + 1>{}, All{});
+  step(std::integral_constant<int, kDppRowShr + 2>{}, All{});
+  step(std::integral_constant<int, kDppRowShr + 4>{}, All{});
+  step(std::integral_constant<int, kDppRowShr + 8>{}, All{});
+  step(std::integral_constant<int, kDppBcast15>{}, std::integral_constant<int, 0xa>{});
+  step(std::integral_constant<int, kDppBcast31>{}, std::integral_constant<int, 0xc>{});
+  return x;
+}
+
+// Maximum over a row of 16 lanes, in its last lane.
+__device__ __forceinline__ float row_max(float x) {
+  const int none = (int)0xff800000;
+  auto step = [&](auto ctrl) __attribute__((always_inline)) {
+    x = fmaxf(x, __builtin_bit_cast(float, dpp_mov<decltype(ctrl)::value, 0xf>(none, __builtin_bit_cast(int, x))));
+  };
+  step(std::integral_constant<int, kDppRowShr + 1>{});
+  step(std::integral_constant<int, kDppRowShr + 2>{});
+  step(std::integral_constant<int, kDppRowShr + 4>{});
+  step(std::integral_constant<int, kDppRowShr + 8>{});
+  return x;
+}
+
+// Sum over the workgroup of everything up to and with this thread, and the total; D is u64 or double.  Fixed order.
+template <int T, class D>
 __device__ __forceinline__ D block_scan(D x, D* part, D& total) {
+  constexpr int W = T / kWave;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const D o = __shfl_up(x, d);
-    if (lane >= d) x += o;
-  }
-  __syncthreads();
+  x = wave_scan64(x);
+  lds_barrier();
   if (lane == 63) part[wave] = x;
-  __syncthreads();
-  D before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w == wave) before = all;
-    all += part[w];
-  }
-  total = all;
-  return before + x;
+  lds_barrier();
+  const D sums = wave_scan64(lane < W ? part[lane < W ? lane : 0] : D(0));
+  auto of_lane = [&](int l) __attribute__((always_inline)) -> D {
+    const u64 b = __builtin_bit_cast(u64, sums);
+    const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)b, l), hi = __builtin_amdgcn_readlane((int)(unsigned)(b >> 32), l);
+    return __builtin_bit_cast(D, (u64)hi << 32 | lo);
+  };
+  total = of_lane(W - 1);
+  const int w = __builtin_amdgcn_readfirstlane(wave);
+  return w ? of_lane(w - 1) + x : x;
 }
 
 template <bool BF16>
 struct Row {
   const void* x;
   float* out;      // or NULL
-  int V, head;     // vector j holds tokens 4 j - head ..
+  int V, head;     // vector j holds tokens 4 j - head .. ; a token's position is its id + head
   float inv_tau;
   bool out_wide;
 
@@ -86,6 +144,7 @@ struct Row {
     return f * inv_tau + 0.f;  // -0 is 0
   }
   __device__ __forceinline__ int vectors() const { return (V + head + 3) >> 2; }
+  __device__ __forceinline__ int position(int v) const { return v + head; }
   // Tokens 4 j - head + {0, 1, 2, 3}; those outside of the row as -inf.
   __device__ __forceinline__ void load(int j, float (&y)[4]) const {
     const int v = 4 * j - head;
@@ -105,9 +164,13 @@ struct Row {
       for (int i = 0; i < 4; ++i) y[i] = v + i >= 0 && v + i < V ? at(v + i) : -INFINITY;
     }
   }
+  // STREAM: many rows, whose outputs only push the logits out of the caches (512 rows of V = 151936 245 -> 228 us)
+  template <bool STREAM>
   __device__ __forceinline__ void store(int v, const float (&y)[4]) const {
     if (out_wide && v >= 0 && v + 4 <= V) {
-      *reinterpret_cast<float4*>(out + v) = make_float4(y[0], y[1], y[2], y[3]);
+      const floatx4 x{y[0], y[1], y[2], y[3]};
+      if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<floatx4*>(out + v));
+      else *reinterpret_cast<floatx4*>(out + v) = x;
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -116,30 +179,63 @@ struct Row {
   }
 };
 
-// All tokens of a row, four at a time: f(first id, y[4]); ids outside of the row come as -inf.  Wavefronts stay whole.
-template <bool BF16, class F>
-__device__ __forceinline__ void each(const Row<BF16>& r, F f) {
-  const int n = r.vectors(), lane = threadIdx.x & 63;
-  for (int j0 = threadIdx.x - lane; j0 < n; j0 += 4 * T) {
-    float y[4][4];
+// Tokens of vectors [begin, end) of a row, four at a time: f(first id, y[4]); ids outside of the row come as -inf, and so do those of vectors
+// that are not wanted.  Wavefronts stay whole.
+template <int T, int U, bool BF16, class F, class W>
+__device__ __forceinline__ void each(const Row<BF16>& r, int begin, int end, F f, W wanted) {
+  const int lane = threadIdx.x & 63;
+  for (int j0 = begin + (int)threadIdx.x - lane; j0 < end; j0 += U * T) {
+    float y[U][4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (j0 + u * T < n) r.load(j0 + u * T + lane, y[u]);
+    for (int u = 0; u < U; ++u)
+      if (j0 + u * T < end) {
+        if (wanted(j0 + u * T + lane)) r.load(j0 + u * T + lane, y[u]);
+        else y[u][0] = y[u][1] = y[u][2] = y[u][3] = -INFINITY;
+      }
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (j0 + u * T < n) f(4 * (j0 + u * T + lane) - r.head, y[u]);
+    for (int u = 0; u < U; ++u)
+      if (j0 + u * T < end) f(4 * (j0 + u * T + lane) - r.head, y[u]);
   }
 }
+template <int T, int U, bool BF16, class F>
+__device__ __forceinline__ void each(const Row<BF16>& r, int begin, int end, F f) { each<T, U>(r, begin, end, f, [](int) { return true; }); }
+template <int T, bool BF16, class F>
+__device__ __forceinline__ void each(const Row<BF16>& r, F f) { each<T, 4>(r, 0, r.vectors(), f); }
 
+// Bins of width 1/32, the middle one from `ref` on, which is at most the row's maximum.  place(y), in 64 bits: the bin and how far y lies in it.
 struct Bins {
-  float ref;
-  __device__ __forceinline__ int of(float y) const { return (int)fminf(fmaxf((y - ref) * kWidth + kBins / 2, 0.f), kBins - 1.f); }
-  __device__ __forceinline__ double middle(int b) const { return (double)ref + ((b - kBins / 2) + 0.5) * (1.0 / kWidth); }
-  // exp(y - middle of its bin)
-  __device__ __forceinline__ double weight(float y, int b) const {
-    const double t = (double)y - middle(b);
-    if (fabs(t) > 1.0 / 63) return exp(t);  // the lowest bin has no lower end
-    return 1.0 + t * (1.0 + t * (1.0 / 2 + t * (1.0 / 6 + t * (1.0 / 24 + t * (1.0 / 120)))));
+  double ref;
+  __device__ __forceinline__ double place(float y) const { return fma((double)y - ref, (double)kWidth, kBins / 2.0); }
+  // whether a maximum lies in them, and 64 above the lowest one
+  __device__ __forceinline__ bool serve(float top) const { return place(top) >= kBins / 2 && place(top) < kBins - 1; }
+  // (the conversion saturates, and gives 0 for NaN; as assembly because the language leaves that open)
+  __device__ __forceinline__ static int of_place(double u) {
+    int b;
+    asm("v_cvt_i32_f64 %0, %1" : "=v"(b) : "v"(u));
+    return min(max(b, 0), kBins - 1);
+  }
+  __device__ __forceinline__ int of(float y) const { return of_place(place(y)); }
+  __device__ __forceinline__ double begin(int b) const { return ref + (b - kBins / 2) * (1.0 / kWidth); }
+  __device__ __forceinline__ double middle(int b) const { return ref + ((b - kBins / 2) + 0.5) * (1.0 / kWidth); }
+  // exp(y - middle of its bin), bins above the lowest: the Taylor polynomial about the middle, in the fraction of u
+  __device__ __forceinline__ static double weight(double u) {
+    const double t = __builtin_amdgcn_fract(u);
+    return horner(t, horner(t, horner(t, horner(t, horner(t, 0x1.1111111111111p-32, 0x1.5p-25), 0x1.500aaaaaaaaabp-18), 0x1.f80feaaaaaaabp-12),
+                            0x1.f80feacp-6), 0x1.f80feabfeeeefp-1);
+  }
+  __device__ __forceinline__ double weight(float y) const { return weight(place(y)); }
+};
+
+// Weights in [0, 4) as whole numbers of 2^-f: adding 2^(52 - f) leaves them in the low bits.
+struct Fixed {
+  double scale, magic;
+  __device__ __forceinline__ explicit Fixed(int V) {
+    const int f = min(50, 61 - (32 - __clz(V)));
+    scale = ldexp(1.0, f);
+    magic = ldexp(1.0, 52 - f);
+  }
+  __device__ __forceinline__ u64 of(double w) const {
+    return __builtin_bit_cast(u64, w + magic) & ((1ull << 52) - 1);
   }
 };
 
@@ -147,49 +243,62 @@ struct Limits {
   unsigned k;      // 0: none
   double p;        // >= 1: none
   unsigned least;  // smallest key that min-p keeps
+  float min_p;     // 0: none
+  bool law;
+};
+
+struct Zone {
+  int bin_k;          // bin where top-k ends, -1: it does not
+  int p_low, p_high;  // bins where top-p can end
+  int sure;           // bins above are kept whole
+  int zone;           // there are tokens to be looked at one by one
+  double above_k;     // mass above bin_k, or all of it
+  __device__ __forceinline__ bool in_k(int bin) const { return bin == bin_k; }
+  __device__ __forceinline__ bool in_p(int bin) const { return bin >= p_low && bin <= p_high; }
 };
 
 // Which of the tokens that `in` admits is the last one: the need_n-th in the order, or, where by_mass, the first at which their mass
 // (relative to exp(top)) reaches need_m.  Readings of the row narrow its key down; `ids` is how many of that key belong to it.
-template <bool BF16, class In>
-__device__ void narrow(Shared& s, const Row<BF16>& r, In in, bool by_mass, u64 need_n, double need_m, float top, double scale,
+template <int T, bool BF16, class In>
+__device__ void narrow(Shared& s, const Row<BF16>& r, In in, bool by_mass, u64 need_n, double need_m, float top, const Fixed& fixed,
                        unsigned& last, unsigned& ids) {
+  constexpr int kPer = kBins / T;
   unsigned low = 0, bits = 32;
   while (bits) {
     const unsigned shift = bits > 12 ? bits - 12 : 0;
-    __syncthreads();
+    lds_barrier();
     for (int b = threadIdx.x; b < kBins; b += T) {
       s.cnt[b] = 0;
       s.mass[b] = 0;
     }
-    __syncthreads();
-    each(r, [&](int, const float(&y)[4]) {
+    lds_barrier();
+    each<T>(r, [&](int, const float(&y)[4]) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const unsigned k = key_of(y[i]);
         if (y[i] >= kNone && in(y[i]) && (bits == 32 || (k - low) >> bits == 0)) {
           const unsigned b = (k - low) >> shift;
           atomicAdd(&s.cnt[b], 1u);
-          if (by_mass) atomicAdd(&s.mass[b], (u64)(exp((double)y[i] - (double)top) * scale + 0.5));
+          if (by_mass) atomicAdd(&s.mass[b], fixed.of(exp64((double)y[i] - (double)top, s.power)));
         }
       }
     });
-    __syncthreads();
-    // from the top: thread t has bins kBins - 1 - 4 t and the three below
+    lds_barrier();
+    // from the top: thread t has bins kBins - 1 - kPer t and the next below
     u64 c = 0, all;
     u64 m = 0, all_m;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int b = kBins - 1 - 4 * (int)threadIdx.x - i;
+    for (int i = 0; i < kPer; ++i) {
+      const int b = kBins - 1 - kPer * (int)threadIdx.x - i;
       c += s.cnt[b];
       m += s.mass[b];
     }
-    u64 c_at = block_scan(c, s.part, all) - c, m_at = block_scan(m, s.part, all_m) - m;
+    u64 c_at = block_scan<T>(c, s.part, all) - c, m_at = block_scan<T>(m, s.part, all_m) - m;
     if (threadIdx.x == 0) s.found[0] = 0;
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int b = kBins - 1 - 4 * (int)threadIdx.x - i;
+    for (int i = 0; i < kPer; ++i) {
+      const int b = kBins - 1 - kPer * (int)threadIdx.x - i;
       const u64 m_next = m_at + s.mass[b], c_next = c_at + s.cnt[b];
       // exactly one bin; the last one with tokens where rounding leaves the mass short
       if (s.cnt[b] && (by_mass ? (double)m_at < need_m && ((double)m_next >= need_m || c_next == all) : c_at < need_n && c_next >= need_n)) {
@@ -200,7 +309,7 @@ __device__ void narrow(Shared& s, const Row<BF16>& r, In in, bool by_mass, u64 n
       m_at = m_next;
       c_at = c_next;
     }
-    __syncthreads();
+    lds_barrier();
     if (by_mass) need_m -= (double)s.sum;
     else need_n -= s.sum;
     low += s.found[0] << shift;
@@ -209,491 +318,1000 @@ __device__ void narrow(Shared& s, const Row<BF16>& r, In in, bool by_mass, u64 n
   last = low;
   const unsigned ties = s.found[1];
   if (by_mass) {
-    const double w = floor(exp((double)of_key(low) - (double)top) * scale + 0.5);
+    const double w = (double)fixed.of(exp64((double)of_key(low) - (double)top, s.power));
     const double n = w > 0 ? ceil(need_m / w) : 1.0;
     ids = n < 1 ? 1 : n > ties ? ties : (unsigned)n;
   } else {
     ids = (unsigned)need_n;
   }
-  __syncthreads();
+  lds_barrier();
 }
 
+// What a row asks for.
 template <bool BF16>
-__device__ void draw_row(const DrawArgs& a, int row, Shared& s) {
+__device__ __forceinline__ void set_up(const DrawArgs& a, int row, Row<BF16>& r, Limits& lim) {
   const int b = row / a.K, m = row - b * a.K;
-  const int tid = threadIdx.x;
-  Row<BF16> r;
   r.V = a.V;
   const long at = (long)b * a.seq_stride + (long)m * a.slot_stride;
   r.x = BF16 ? (const void*)((const __bf16*)a.logits + at) : (const void*)((const float*)a.logits + at);
   r.head = (int)(((uintptr_t)r.x / (BF16 ? 2 : 4)) & 3);
   r.out = a.out ? a.out + (long)b * a.out_seq_stride + (long)m * a.out_slot_stride : nullptr;
   r.out_wide = (((uintptr_t)r.out - 4 * (uintptr_t)r.head) & 15) == 0;
-  float tau_inv = a.inv_tau;
-  Limits lim;
   lim.k = a.top_k && a.top_k[b] > 0 ? (unsigned)a.top_k[b] : 0;
   lim.p = a.top_p && a.top_p[b] < 1.f ? (double)a.top_p[b] : 2.0;
-  const float min_p = a.min_p && a.min_p[b] > 0.f ? a.min_p[b] : 0.f;
-  bool law = true;
+  lim.min_p = a.min_p && a.min_p[b] > 0.f ? a.min_p[b] : 0.f;
+  lim.least = 0;
+  lim.law = true;
+  r.inv_tau = a.inv_tau;
   if (a.temperatures) {
     const float t = a.temperatures[b];
-    law = t >= 0.f;
-    tau_inv = 1.f / t;
-    if (!(tau_inv < INFINITY)) {
-      tau_inv = 1.f;
+    lim.law = t >= 0.f;
+    r.inv_tau = 1.f / t;
+    if (!(r.inv_tau < INFINITY)) {
+      r.inv_tau = 1.f;
       lim.k = 1;
     }
   }
-  r.inv_tau = tau_inv;
-  if (lim.p <= 0 || min_p > 1.f) lim.k = 1;
-  if (lim.k == 1 || lim.p <= 0) lim.p = 2.0;
-  const bool by_k = lim.k > 0, by_p = lim.p < 1;
+  if (lim.p <= 0 || lim.min_p > 1.f) lim.k = 1;
+  if (lim.k == 1) lim.p = 2.0;
+}
+__device__ __forceinline__ bool by_k(const Limits& l) { return l.k > 0; }
+__device__ __forceinline__ bool by_p(const Limits& l) { return l.p < 1; }
 
-  // 1. maximum and bins
-  Bins bins{0.f};
-  float top = 0.f;
-  const int log_v = 32 - __clz(a.V);  // V < 2^log_v
-  const double scale = __builtin_ldexp(1.0, 61 - log_v);
-  for (int turn = 0;; ++turn) {
-    __syncthreads();
-    if (by_k || by_p)
-      for (int i = tid; i < kBins; i += T) {
-        s.cnt[i] = 0;
-        s.mass[i] = 0;
+__device__ __forceinline__ void set_powers(Shared& s) {
+  if (threadIdx.x < 64) s.power[threadIdx.x] = exp2(threadIdx.x * (1.0 / 64));
+}
+
+// Step 1 over vectors [begin, end): s.cnt, s.mass (zero before), in each thread its largest y, NaN if there is one, and the largest of each group of
+// 64 positions.
+template <int T, bool GROUPS = false, bool BF16>
+__device__ __forceinline__ void count(Shared& s, const Row<BF16>& r, int begin, int end, const Limits& lim, const Bins& bins, const Fixed& fixed,
+                                      float& high, float* groups = nullptr) {
+  unsigned low = 0;
+  auto run = [&](auto k_tag, auto p_tag) __attribute__((always_inline)) {
+    each<T, GROUPS ? 4 : 8>(r, begin, end, [&](int v, const float(&y)[4]) __attribute__((always_inline)) {
+      const float four = __builtin_elementwise_maximum(__builtin_elementwise_maximum(y[0], y[1]), __builtin_elementwise_maximum(y[2], y[3]));
+      high = __builtin_elementwise_maximum(high, four);
+      if constexpr (GROUPS) {
+        const float of_row = row_max(four);
+        const int group = r.position(v) >> kGroupLog;
+        if ((threadIdx.x & 15) == 15 && group < kGroups) groups[group] = of_row;
       }
-    if (tid == 0) {
-      s.found[0] = 0;
-      s.found[1] = 0;
-      s.list_n = 0;
-      s.kept = 0;
-    }
-    for (int i = tid; i < kTiles; i += T) s.tile[i] = 0;
-    __syncthreads();
-    unsigned high = 0;
-    bool bad = false;
-    each(r, [&](int, const float(&y)[4]) {
+      if constexpr (decltype(k_tag)::value || decltype(p_tag)::value) {
+        double u[4];
+        int bin[4];
+        u64 w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bad |= !(y[i] < INFINITY);
-        if (y[i] >= kNone) {
-          high = max(high, key_of(y[i]));
-          if (y[i] < INFINITY) {
-            if (by_k | by_p) {
-              const int bin = bins.of(y[i]);
-              if (by_k) atomicAdd(&s.cnt[bin], 1u);
-              if (by_p) atomicAdd(&s.mass[bin], (u64)(bins.weight(y[i], bin) * scale + 0.5));
-            }
+        for (int i = 0; i < 4; ++i) u[i] = bins.place(y[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bin[i] = Bins::of_place(u[i]);
+        if constexpr (decltype(p_tag)::value)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = fixed.of(Bins::weight(u[i]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (bin[i] > 0) {
+            if constexpr (decltype(k_tag)::value) atomicAdd(&s.cnt[bin[i]], 1u);
+            if constexpr (decltype(p_tag)::value) atomicAdd(&s.mass[bin[i]], w[i]);
+          } else if constexpr (decltype(k_tag)::value) {
+            low += y[i] >= kNone;
           }
         }
       }
     });
-    atomicMax(&s.found[0], high);
-    if (bad) s.found[1] = 1;
-    __syncthreads();
-    const unsigned top_key = s.found[0];
-    law = law && top_key && !s.found[1];
-    if (!law) break;
-    top = of_key(top_key);
-    if (turn || !(by_k || by_p) || (top >= -32.f && top < 62.f)) break;
-    bins.ref = top - 62.f;
-  }
-  if (!law) {  // nothing kept
-    if (r.out) {
-      const float none[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      const int n = r.vectors();
-      for (int j = tid; j < n; j += T) r.store(4 * j - r.head, none);
-    }
-    if (tid == 0) {
-      if (a.out_tokens) a.out_tokens[row] = -1;
-      if (a.out_conf) a.out_conf[row] = 0.f;
-      if (a.out_kept) a.out_kept[row] = 0;
-      if (a.out_lse) a.out_lse[row] = -INFINITY;
-    }
-    return;
-  }
-  // min-p as a key: the smallest y with exp(y - top) >= min_p
-  lim.least = 0;
-  if (min_p > 0.f && min_p <= 1.f) {
-    const auto keeps = [&](unsigned k) { return exp((double)of_key(k) - (double)top) >= (double)min_p; };
-    const double near = (double)top + log((double)min_p);
-    unsigned low = key_of((float)(near - 0.01)), k = key_of(fminf((float)(near + 0.01), top));
-    if (!keeps(k)) ++k;  // (numbers so far apart that one step misses the border)
-    if (keeps(low)) k = low;
-    while (k - low > 1 && k != low) {
-      const unsigned mid = low + (k - low) / 2;
-      if (keeps(mid)) k = mid;
-      else low = mid;
-    }
-    lim.least = k;
-  }
+  };
+  using Yes = std::true_type;
+  using No = std::false_type;
+  if (by_k(lim) && by_p(lim)) run(Yes{}, Yes{});
+  else if (by_k(lim)) run(Yes{}, No{});
+  else if (by_p(lim)) run(No{}, Yes{});
+  else run(No{}, No{});
+  if (low) atomicAdd(&s.cnt[0], low);
+}
 
-  // 2. where top-k and top-p end.  Zone: bins whose tokens have to be looked at one by one.
-  int bin_k = -1, p_low = kBins, p_high = -1;  // -1: all of the row; zone of top-p: p_low .. p_high
-  double above_k = 0;
-  if (by_k || by_p) {
-    unsigned c = 0;
-    double w = 0, wi[4];
-    unsigned ci[4];
+// min-p as a key: the smallest y with exp(y - top) >= min_p.
+__device__ __forceinline__ void set_least(Limits& lim, float top) {
+  if (!(lim.min_p > 0.f && lim.min_p <= 1.f)) return;
+  const auto keeps = [&](unsigned k) { return exp((double)of_key(k) - (double)top) >= (double)lim.min_p; };
+  const double near = (double)top + log((double)lim.min_p);
+  const unsigned guess = key_of((float)near);
+  unsigned low = guess - 2, k = min(guess + 2, key_of(top));
+  if (!keeps(k) || keeps(low)) {  // sums near 0 may be further off; and numbers may be so far apart that one step misses the border
+    low = key_of((float)(near - 0.01));
+    k = key_of(fminf((float)(near + 0.01), top));
+    if (!keeps(k)) ++k;
+    if (keeps(low)) k = low;
+  }
+  while (k - low > 1 && k != low) {
+    const unsigned mid = low + (k - low) / 2;
+    if (keeps(mid)) k = mid;
+    else low = mid;
+  }
+  lim.least = k;
+}
+
+// Step 2 over the PER T bins from b0 down: s.cnt and s.mass become what lies above each of them.  all, total: tokens and mass of the row, or
+// (BELOW) of its bins further down; FULL: there are none.  False: the limits end below these bins.
+template <int T, int PER, bool FULL, bool BELOW>
+__device__ __forceinline__ bool find_zone(Shared& s, const Limits& lim, const Bins& bins, float top, int b0, u64 all, double total, Zone& z) {
+  z = Zone{-1, kBins, -1, -1, 0, 0};
+  const int tid = threadIdx.x;
+  if (!by_k(lim) && !by_p(lim)) return true;
+  unsigned c = 0, ci[PER];
+  double w = 0, wi[PER];
+  u64 mi[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int bin = b0 - PER * tid - i;
+    ci[i] = by_k(lim) && bin >= 0 ? s.cnt[bin] : 0;
+    mi[i] = by_p(lim) && bin > 0 ? s.mass[bin] : 0;
+    c += ci[i];
+  }
+  u64 any = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    any |= mi[i];
+    wi[i] = 0;
+  }
+  if (__ballot(any != 0)) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      wi[i] = (double)mi[i] * exp64(bins.middle(b0 - PER * tid - i) - (double)top, s.power);  // of 2^-f
+      w += wi[i];
+    }
+  }
+  u64 c_here = 0, c_at = 0;
+  double w_here = 0, w_at = 0;
+  if (by_k(lim)) c_at = block_scan<T>((u64)c, s.part, c_here) - c;
+  if (by_p(lim)) w_at = block_scan<T>(w, (double*)s.part, w_here) - w;
+  if (FULL || BELOW) {
+    all += c_here;
+    total += w_here;
+  }
+  if (tid == 0) s.found[0] = s.found[1] = s.found[2] = 0xffffffffu;
+  lds_barrier();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int bin = b0 - PER * tid - i;
+    if (by_k(lim) && c_at < lim.k && c_at + ci[i] >= lim.k && lim.k < all) {
+      s.found[0] = bin;
+      s.value[0] = w_at;
+      s.value[1] = w_at + wi[i];
+    }
+    if (bin >= 0) {
+      s.cnt[bin] = (unsigned)c_at;
+      s.mass[bin] = __builtin_bit_cast(u64, w_at);
+    }
+    c_at += ci[i];
+    w_at += wi[i];
+  }
+  lds_barrier();
+  const bool ends = s.found[0] != 0xffffffffu;
+  bool here = ends || !by_k(lim) || lim.k >= all;
+  z.bin_k = ends ? (int)s.found[0] : -1;
+  z.above_k = ends ? s.value[0] : total;
+  if (by_p(lim)) {
+    // with the mass top-k leaves somewhere in [lowest, highest], and a little room for the sums' rounding
+    const double lowest = lim.p * z.above_k * (1 - 1e-12), highest = lim.p * (ends ? s.value[1] : total) * (1 + 1e-12);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int bin = b0 - PER * tid - i;
+      if (!(wi[i] > 0)) continue;
+      const double before = __builtin_bit_cast(double, s.mass[bin]);
+      if ((before < lowest || before == 0) && before + wi[i] >= lowest) atomicMin(&s.found[1], (unsigned)(kBins - 1 - bin));  // may be the first to reach it
+      if (before < highest && before + wi[i] >= highest) atomicMin(&s.found[2], (unsigned)bin);                               // the last that may be needed
+    }
+    lds_barrier();
+    here = here && (FULL || (s.found[1] != 0xffffffffu && s.found[2] != 0xffffffffu));
+    z.p_high = s.found[1] == 0xffffffffu ? kBins - 1 : kBins - 1 - (int)s.found[1];
+    z.p_low = s.found[2] == 0xffffffffu ? 0 : (int)s.found[2];
+    if (ends && z.p_low < z.bin_k) z.p_low = z.bin_k;
+    if (ends && z.p_high < z.bin_k) z.p_high = z.bin_k;
+  }
+  z.sure = by_p(lim) ? z.p_high : z.bin_k;
+  z.zone = by_p(lim) || z.bin_k >= 0;
+  if (tid == 0 && z.bin_k >= 0) s.above_k = s.cnt[z.bin_k];
+  return here;
+}
+
+// Step 3 over vectors [begin, end): out, s.tile, s.list, s.list_n (which counts on where the list is full).  Returns the tokens kept (of this
+// thread).
+template <int T, bool GROUPS = false, bool BF16>
+__device__ __forceinline__ unsigned keep(Shared& s, const Row<BF16>& r, int begin, int end, const Limits& lim, const Bins& bins, const Fixed& fixed,
+                                         const Zone& z, float top, int tile_log, const float* groups = nullptr) {
+  // y from `sure` on is kept, y below `maybe` is not; in between the bins say (and a little beside the zone, whose borders are numbers of 64 bits)
+  const float least = fmaxf(kNone, lim.least ? of_key(lim.least) : kNone);
+  const int low_bin = by_p(lim) ? (z.bin_k >= 0 ? min(z.bin_k, z.p_low) : z.p_low) : z.bin_k;
+  const double up = z.zone ? bins.begin(z.sure + 1) : 0, down = z.zone ? bins.begin(low_bin) : 0;
+  const float sure = z.zone ? (z.sure < kBins - 1 ? fmaxf((float)(up + (1e-6 + 1e-6 * fabs(up))), least) : INFINITY) : least;
+  const float maybe = z.zone ? (low_bin > 0 ? (float)(down - (1e-6 + 1e-6 * fabs(down))) : kNone) : INFINITY;
+  const float wanted = fminf(sure, maybe);
+  unsigned kept = 0;
+  each<T, 4>(r, begin, end, [&](int v, const float(&y)[4]) __attribute__((always_inline)) {
+    float o[4];
+    bool any = false, listed = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int bin = kBins - 1 - 4 * tid - i;
-      ci[i] = s.cnt[bin];
-      wi[i] = s.mass[bin] ? (double)s.mass[bin] * exp(bins.middle(bin) - (double)top) : 0;  // of 2^-s
-      c += ci[i];
-      w += wi[i];
+      const bool keep = y[i] >= sure;
+      o[i] = keep ? y[i] : -INFINITY;
+      any |= keep;
+      listed |= y[i] >= maybe && !keep;
+    }
+    if (listed) {
+      bool is[4];
+      unsigned n = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int bin = bins.of(y[i]);
+        const bool token = y[i] >= maybe && y[i] >= kNone && !(y[i] >= sure);
+        is[i] = token && (z.in_k(bin) || (by_p(lim) && z.in_p(bin)));
+        n += is[i];
+        if (token && bin > z.sure && y[i] >= least) {
+          o[i] = y[i];
+          any = true;
+        }
+      }
+      if (n) {
+        unsigned p = atomicAdd(&s.list_n, n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (is[i]) {
+            if (p < kList) s.list[p] = ((u64)key_of(y[i]) << 32) | (unsigned)~(v + i);
+            ++p;
+          }
+      }
+    }
+    if (__ballot(any)) {
+      u64 w[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[i] = o[i] > -INFINITY ? fixed.of(exp64((double)o[i] - (double)top, s.power)) : 0;
+        kept += o[i] > -INFINITY;
+        sum += w[i];
+      }
+      const int p0 = r.position(v) - 4 * (int)(threadIdx.x & 63);  // of the wavefront
+      if (p0 >> tile_log == (p0 + 255) >> tile_log) {
+        sum = wave_scan64(sum);
+        if ((threadIdx.x & 63) == 63 && sum) atomicAdd(&s.tile[p0 >> tile_log], sum);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (w[i]) atomicAdd(&s.tile[r.position(v + i) >> tile_log], w[i]);
+      }
+    }
+    if (r.out) r.template store<GROUPS>(v, o);
+  }, [&](int j) __attribute__((always_inline)) {
+    if constexpr (!GROUPS) return true;
+    const int group = (4 * j) >> kGroupLog;
+    return group >= kGroups || groups[group] >= wanted;
+  });
+  return kept;
+}
+
+// Step 4: the last token kept, from n <= kList entries of s.list.  Adds what the list keeps to s.tile and s.kept, and writes it.
+template <int T, bool BF16>
+__device__ __forceinline__ void resolve(Shared& s, const Row<BF16>& r, const Limits& lim, const Bins& bins, const Fixed& fixed, const Zone& z,
+                                        float top, int tile_log, unsigned n, unsigned& last, int& last_id) {
+  const int tid = threadIdx.x;
+  unsigned size = 2;
+  while (size < n) size <<= 1;
+  for (unsigned i = n + tid; i < size; i += T) s.list[i] = 0;
+  lds_barrier();
+  auto exchange = [&](unsigned i, unsigned k, unsigned d) __attribute__((always_inline)) {
+    const unsigned x = 2 * i - (i & (d - 1)), y = x + d;
+    const u64 p = s.list[x], q = s.list[y];
+    if ((p < q) == ((x & k) == 0)) {  // descending
+      s.list[x] = q;
+      s.list[y] = p;
+    }
+  };
+  if (size <= 128) {  // one wavefront, whose LDS operations keep their order
+    if (tid < 64)
+      for (unsigned k = 2; k <= size; k <<= 1)
+        for (unsigned d = k >> 1; d; d >>= 1) {
+          if (tid < (int)size / 2) exchange(tid, k, d);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+    lds_barrier();
+  } else {
+    for (unsigned k = 2; k <= size; k <<= 1)
+      for (unsigned d = k >> 1; d; d >>= 1) {
+        for (unsigned i = tid; i < size / 2; i += T) exchange(i, k, d);
+        lds_barrier();
+      }
+  }
+  auto y_of = [&](unsigned i) __attribute__((always_inline)) { return of_key((unsigned)(s.list[i] >> 32)); };
+  // sums[i]: weights of the entries in front of entry i, each relative to its own bin's middle; thread t has `per` neighbours
+  u64* const sums = reinterpret_cast<u64*>(s.cnt);
+  static_assert(sizeof s.cnt >= kList * sizeof(u64), "");
+  const unsigned per = (n + T - 1) / T, i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  if (by_p(lim)) {
+    u64 mine = 0, all;
+    for (unsigned i = i0; i < i1; ++i) {
+      mine += fixed.of(bins.weight(y_of(i)));
+    }
+    u64 before = block_scan<T>(mine, s.part, all) - mine;
+    for (unsigned i = i0; i < i1; ++i) {
+      sums[i] = before;
+      before += fixed.of(bins.weight(y_of(i)));
+    }
+    if (tid == 0) s.last_sum = all;
+    lds_barrier();
+  }
+  // first entry of a bin or a lower one
+  auto begin_of = [&](int bin) __attribute__((always_inline)) {
+    unsigned lo = 0, hi = n;
+    while (lo < hi) {
+      const unsigned mid = (lo + hi) / 2;
+      if (bins.of(y_of(mid)) > bin) lo = mid + 1;
+      else hi = mid;
+    }
+    return lo;
+  };
+  double target = INFINITY;
+  unsigned k_first = 0, k_end = n;  // entries of bin_k that top-k leaves end at k_end
+  if (z.bin_k >= 0) {
+    k_first = begin_of(z.bin_k);
+    k_end = min(n, k_first + (lim.k - s.above_k));
+  }
+  if (by_p(lim)) {
+    double left = z.above_k;
+    if (z.bin_k >= 0) left += (double)((k_end < n ? sums[k_end] : s.last_sum) - sums[k_first]) * exp64(bins.middle(z.bin_k) - (double)top, s.power);
+    target = lim.p * kReached * left;
+  }
+  unsigned mine = 0;
+  for (unsigned i = i0; i < min(i1, k_end); ++i) {
+    const float y = y_of(i);
+    bool is = key_of(y) >= lim.least;
+    if (by_p(lim)) {
+      const int bin = bins.of(y);
+      is = is && __builtin_bit_cast(double, s.mass[bin]) + (double)(sums[i] - sums[begin_of(bin)]) * exp64(bins.middle(bin) - (double)top, s.power) < target;
+    }
+    mine += is;
+  }
+  u64 kept;
+  block_scan<T>((u64)mine, s.part, kept);
+  last_id = 0x7fffffff;
+  if (kept) {
+    const u64 e = s.list[kept - 1];
+    last = (unsigned)(e >> 32);
+    last_id = (int)~(unsigned)e;
+  } else {
+    last = (unsigned)(s.list[0] >> 32) + 1;
+  }
+  __syncthreads();  // waits for the stores of step 3 too, some of which these overwrite
+  for (unsigned i = tid; i < kept; i += T) {
+    const float y = y_of(i);
+    const int id = (int)~(unsigned)s.list[i];
+    const u64 e = fixed.of(exp64((double)y - (double)top, s.power));
+    if (e) atomicAdd(&s.tile[r.position(id) >> tile_log], e);
+    if (r.out) r.out[id] = y;
+  }
+  if (tid == 0) s.kept += (unsigned)kept;
+  lds_barrier();
+}
+
+// Step 4 by readings of the row, from step 2 over all bins.
+template <int T, bool BF16>
+__device__ __forceinline__ void resolve_by_reading(Shared& s, const Row<BF16>& r, const Limits& lim, const Bins& bins, const Fixed& fixed, const Zone& z, float top,
+                                   int tile_log, unsigned& last, int& last_id) {
+  const int tid = threadIdx.x;
+  const double above_p = by_p(lim) ? __builtin_bit_cast(double, s.mass[z.p_high]) : 0;
+  const unsigned c_k = z.bin_k >= 0 ? s.cnt[z.bin_k] : 0;
+  lds_barrier();
+  unsigned ids = 0xffffffffu;  // how many tokens of key `last` are kept
+  double left = z.above_k;
+  last = 0;
+  auto in_k = [&](float y) { return z.in_k(bins.of(y)); };
+  auto in_p = [&](float y) { return z.in_p(bins.of(y)); };
+  if (z.bin_k >= 0) {
+    narrow<T>(s, r, in_k, false, (u64)(lim.k - c_k), 0.0, top, fixed, last, ids);
+    if (by_p(lim) && z.bin_k > 0) {
+      // mass of what top-k keeps of its bin
+      u64 mine = 0, in_bin;
+      each<T>(r, [&](int, const float(&y)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (y[i] >= kNone && in_k(y[i]) && key_of(y[i]) > last) mine += fixed.of(bins.weight(y[i]));
+      });
+      block_scan<T>(mine, s.part, in_bin);
+      const u64 each_w = fixed.of(bins.weight(of_key(last)));
+      left += ((double)in_bin + (double)ids * (double)each_w) * exp64(bins.middle(z.bin_k) - (double)top, s.power);
+    }
+  }
+  if (by_p(lim)) {
+    unsigned last_p, ids_p, high, one;
+    // relative to the zone's largest token, found as the first in its order
+    narrow<T>(s, r, in_p, false, (u64)1, 0.0, top, fixed, high, one);
+    const float high_y = of_key(high);
+    const double need = (lim.p * kReached * left - above_p) / exp64((double)high_y - (double)top, s.power);
+    last_p = high;
+    ids_p = 0;
+    if (need > 0) narrow<T>(s, r, in_p, true, (u64)0, need, high_y, fixed, last_p, ids_p);
+    if (last_p > last || (last_p == last && ids_p < ids)) {
+      last = last_p;
+      ids = ids_p;
+    }
+  }
+  // the id of the last of them
+  lds_barrier();
+  unsigned* const per_tile = s.cnt;
+  for (int i = tid; i < kTiles; i += T) per_tile[i] = 0;
+  lds_barrier();
+  each<T>(r, [&](int v, const float(&y)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (y[i] >= kNone && key_of(y[i]) == last) atomicAdd(&per_tile[r.position(v + i) >> tile_log], 1u);
+  });
+  lds_barrier();
+  if (tid == 0) {
+    s.found[0] = 0xffffffffu;
+    unsigned before = 0;
+    for (int i = 0; i < kTiles; ++i) {
+      if (before < ids && before + per_tile[i] >= ids) { s.found[0] = i; s.found[1] = before; }
+      before += per_tile[i];
+    }
+    s.found[2] = ids ? 0x7fffffffu : 0xffffffffu;
+  }
+  lds_barrier();
+  const unsigned in_tile = s.found[0];
+  if (in_tile != 0xffffffffu) {
+    u64 before = s.found[1];
+    lds_barrier();
+    const int end = min(r.position(r.V), (int)(in_tile + 1) << tile_log);
+    for (int p0 = (int)in_tile << tile_log; p0 < end; p0 += T) {
+      const int v = p0 + tid - r.head;
+      float y = -INFINITY;
+      if (v >= 0 && p0 + tid < end) y = r.at(v);
+      const u64 is = y >= kNone && key_of(y) == last;
+      u64 all;
+      const u64 to = before + block_scan<T>(is, s.part, all);
+      if (is && to == ids) s.found[2] = (unsigned)v;
+      before += all;
+    }
+    lds_barrier();
+  }
+  last_id = (int)s.found[2];
+  // what the zone keeps
+  const int lowest = by_p(lim) ? z.p_low : z.bin_k;
+  unsigned kept = 0;
+  each<T>(r, [&](int v, const float(&y)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (y[i] >= kNone) {
+        const unsigned k = key_of(y[i]);
+        const int bin = bins.of(y[i]);
+        if (bin <= z.sure && bin >= lowest && k >= lim.least && (k > last || (k == last && v + i <= last_id))) {
+          const u64 e = fixed.of(exp64((double)y[i] - (double)top, s.power));
+          if (e) atomicAdd(&s.tile[r.position(v + i) >> tile_log], e);
+          ++kept;
+          if (r.out) r.out[v + i] = y[i];
+        }
+      }
+    }
+  });
+  if (kept) atomicAdd(&s.kept, kept);
+  lds_barrier();
+}
+
+__device__ __forceinline__ void no_token(const DrawArgs& a, int row) {
+  if (threadIdx.x == 0) {
+    if (a.out_tokens) a.out_tokens[row] = -1;
+    if (a.out_conf) a.out_conf[row] = 0.f;
+    if (a.out_kept) a.out_kept[row] = 0;
+    if (a.out_lse) a.out_lse[row] = -INFINITY;
+  }
+}
+// Step 5, from s.tile and s.kept.
+template <int T, bool BF16>
+__device__ __forceinline__ void token(Shared& s, const DrawArgs& a, int row, const Row<BF16>& r, const Limits& lim, const Fixed& fixed, float top,
+                                      int tile_log, unsigned last, int last_id) {
+  constexpr int kPer = (kTiles + T - 1) / T;  // neighbouring tiles per thread
+  const int tid = threadIdx.x;
+  u64 mine = 0, total;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (kPer * tid + i < kTiles) mine += s.tile[kPer * tid + i];
+  u64 to = block_scan<T>(mine, s.part, total) - mine;
+  if (!total) {  // (the row's maximum has the largest weight there is)
+    no_token(a, row);
+    return;
+  }
+  const float u = a.uniforms ? fminf(fmaxf(a.uniforms[row], 0.f), 1.f) : 0.f;
+  const double target = (double)u * (double)total;
+  // the first tile at whose end the mass reaches the target
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const u64 t = kPer * tid + i < kTiles ? s.tile[kPer * tid + i] : 0;
+    if (t && (double)(to + t) >= target && ((double)to < target || to == 0)) {
+      s.found[0] = kPer * tid + i;
+      s.sum = to;
+    }
+    to += t;
+  }
+  if (tid == 0) {
+    s.found[1] = 0x7fffffffu;
+    if (a.out_lse) a.out_lse[row] = (float)((double)top + log((double)total / fixed.scale));
+    if (a.out_kept) a.out_kept[row] = (int)s.kept;
+  }
+  lds_barrier();
+  const int tile = (int)s.found[0];
+  u64 before = s.sum;
+  const int end = min(r.position(r.V), (tile + 1) << tile_log);
+  const float y_last = of_key(last);
+  const float least = fmaxf(kNone, lim.least ? of_key(lim.least) : kNone);
+  for (int p0 = tile << tile_log; p0 < end; p0 += 4 * T) {
+    u64 w[4], sum = 0, all;
+    float y[4];
+    const int v = p0 + 4 * tid - r.head;
+    r.load((p0 >> 2) + tid, y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = 0;
+      if (y[i] >= least && r.position(v + i) < end && (last == 0 || key_of(y[i]) > last || (y[i] == y_last && v + i <= last_id)))
+        w[i] = fixed.of(exp64((double)y[i] - (double)top, s.power));
+      sum += w[i];
+    }
+    u64 to_here = before + block_scan<T>(sum, s.part, all) - sum;
+    // the first token at which the mass reaches the target: what lies in front of it does not
+    bool mine = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool is = w[i] && (double)(to_here + w[i]) >= target && ((double)to_here < target || to_here == 0);
+      if (is) {
+        if (a.out_tokens) a.out_tokens[row] = v + i;
+        if (a.out_conf) a.out_conf[row] = (float)((double)w[i] / (double)total);
+      }
+      mine |= is;
+      to_here += w[i];
+    }
+    if (mine) s.found[1] = 0;
+    before += all;
+    if (p0 + 4 * T >= end) break;
+    lds_barrier();
+    if (s.found[1] == 0) break;
+  }
+}
+
+template <int T, bool BF16>
+__device__ __forceinline__ void no_logits(const Row<BF16>& r, int begin, int end) {
+  if (!r.out) return;
+  const float none[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  for (int j = begin + (int)threadIdx.x; j < end; j += T) r.template store<false>(4 * j - r.head, none);
+}
+
+// The largest y of the workgroup, through s.found[0]; s.found[1]: whether there is a NaN or +inf.  Both 0 before.
+__device__ __forceinline__ float top_of(Shared& s, float high) {
+  if (!(high < INFINITY)) s.found[1] = 1;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) high = fmaxf(high, __shfl_xor(high, d));
+  if ((threadIdx.x & 63) == 0) atomicMax(&s.found[0], key_of(high));
+  lds_barrier();
+  return of_key(s.found[0]);
+}
+
+// Bins of a row by the largest of a sample, a vector per thread in T / 64 places; through s.found[2], which is 0 before.
+template <int T, bool BF16>
+__device__ __forceinline__ Bins bins_of(Shared& s, const Row<BF16>& r) {
+  const int n = r.vectors(), wave = threadIdx.x >> 6;
+  float y[4], high = -INFINITY;
+  r.load((int)((long)n * wave / (T / 64)) + (int)(threadIdx.x & 63), y);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (y[i] < INFINITY) high = fmaxf(high, y[i]);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) high = fmaxf(high, __shfl_xor(high, d));
+  if ((threadIdx.x & 63) == 0) atomicMax(&s.found[2], key_of(high));
+  lds_barrier();
+  const float top = of_key(s.found[2]);
+  return Bins{top >= kNone ? (double)top - 16.0 : 0.0};
+}
+
+template <int T>
+__device__ __forceinline__ void clear(Shared& s) {
+  uint4* const c = reinterpret_cast<uint4*>(s.cnt);
+  uint4* const m = reinterpret_cast<uint4*>(s.mass);
+  const uint4 zero{0, 0, 0, 0};
+  for (int i = threadIdx.x; i < kBins / 4; i += T) c[i] = zero;
+  for (int i = threadIdx.x; i < kBins / 2; i += T) m[i] = zero;
+  for (int i = threadIdx.x; i < kTiles; i += T) s.tile[i] = 0;
+  if (threadIdx.x == 0) s.found[0] = s.found[1] = s.found[2] = s.found[3] = s.list_n = s.kept = 0;
+}
+
+// Tokens and mass (relative to y) of the bins below `end`.
+template <int T>
+__device__ __forceinline__ void totals(Shared& s, const Limits& lim, const Bins& bins, double y, int end, u64& all, double& total) {
+  constexpr int U = 4;
+  unsigned c = 0;
+  double w = 0;
+  for (int b = threadIdx.x; b < end; b += U * T) {
+    unsigned ci[U];
+    u64 wi[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      ci[u] = by_k(lim) && b + u * T < end ? s.cnt[b + u * T] : 0;
+      wi[u] = by_p(lim) && b + u * T < end ? s.mass[b + u * T] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      c += ci[u];
+      if (__ballot(wi[u] != 0)) w += (double)wi[u] * exp64(bins.middle(b + u * T) - y, s.power);
+    }
+  }
+  all = 0;
+  total = 0;
+  if (by_k(lim)) block_scan<T>((u64)c, s.part, all);
+  if (by_p(lim)) block_scan<T>(w, (double*)s.part, total);
+}
+
+__host__ __device__ inline int tile_log_of(int V) {  // tiles of 2^this positions: at least 1024, at most kTiles of them
+  int log = 10;
+  while ((long)V + 3 > (long)kTiles << log) ++log;
+  return log;
+}
+
+// A row that is left: all bins, the middle one 31 below the maximum, and step 4 by readings.
+template <int T, bool BF16>
+__device__ __forceinline__ void left_row(const DrawArgs& a, int row, Shared& s) {
+  Row<BF16> r;
+  Limits lim;
+  set_up(a, row, r, lim);
+  set_powers(s);
+  const Fixed fixed(a.V);
+  const int tile_log = tile_log_of(a.V);
+  lds_barrier();
+  clear<T>(s);
+  lds_barrier();
+  float high = -INFINITY;
+  each<T>(r, [&](int, const float(&y)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) high = fmaxf(high, y[i]);
+  });
+  const float top = top_of(s, high);
+  const Bins bins{(double)top - 31.0};
+  count<T>(s, r, 0, r.vectors(), lim, bins, fixed, high);
+  lds_barrier();
+  set_least(lim, top);
+  Zone z;
+  find_zone<T, kBins / T, true, false>(s, lim, bins, top, kBins - 1, 0, 0.0, z);
+  const unsigned kept = keep<T>(s, r, 0, r.vectors(), lim, bins, fixed, z, top, tile_log);
+  if (kept) atomicAdd(&s.kept, kept);
+  lds_barrier();
+  unsigned last = 0;
+  int last_id = 0x7fffffff;
+  if (z.zone) resolve_by_reading<T>(s, r, lim, bins, fixed, z, top, tile_log, last, last_id);
+  token<T>(s, a, row, r, lim, fixed, top, tile_log, last, last_id);
+}
+
+// All steps for one row.  HERE: also where it is left; else left[row] says whether it is (the registers of what that takes would cost
+// the second workgroup of a CU).
+template <int T, bool BF16, bool HERE>
+__global__ __launch_bounds__(T, HERE ? 1 : 4) void draw_rows_kernel(DrawArgs a, int* left) {
+  constexpr int kWindow = 2048;
+  constexpr bool GROUPS = !HERE;
+  __shared__ Shared s;
+  __shared__ float groups[GROUPS ? kGroups : 1];
+  const int tid = threadIdx.x, row = blockIdx.x;
+  Row<BF16> r;
+  Limits lim;
+  set_up(a, row, r, lim);
+  set_powers(s);
+  const Fixed fixed(a.V);
+  const int tile_log = tile_log_of(a.V);
+  clear<T>(s);
+  lds_barrier();
+  const Bins bins = bins_of<T>(s, r);
+  float high = -INFINITY;
+  count<T, GROUPS>(s, r, 0, r.vectors(), lim, bins, fixed, high, groups);
+  const float top = top_of(s, high);
+  if (!lim.law || !(top >= kNone) || s.found[1]) {
+    no_logits<T>(r, 0, r.vectors());
+    no_token(a, row);
+    if (!HERE && tid == 0) left[row] = 0;
+    return;
+  }
+  set_least(lim, top);
+  Zone z{-1, kBins, -1, -1, 0, 0};
+  bool here = true;
+  if (by_k(lim) || by_p(lim)) {
+    u64 all;
+    double total;
+    const int b0 = bins.of(top);
+    totals<T>(s, lim, bins, top, b0 - kWindow + 1, all, total);
+    here = find_zone<T, kWindow / T, false, true>(s, lim, bins, top, b0, all, total, z) && bins.serve(top);
+    lds_barrier();
+  }
+  if (here) {
+    const unsigned kept = keep<T, GROUPS>(s, r, 0, r.vectors(), lim, bins, fixed, z, top, tile_log, groups);
+    if (kept) atomicAdd(&s.kept, kept);
+    lds_barrier();
+  }
+  here = here && s.list_n <= kList;
+  if (!HERE && tid == 0) left[row] = !here;
+  if (!here) {
+    if constexpr (HERE) left_row<T, BF16>(a, row, s);
+    return;
+  }
+  unsigned last = 0;
+  int last_id = 0x7fffffff;
+  if (z.zone) resolve<T>(s, r, lim, bins, fixed, z, top, tile_log, s.list_n, last, last_id);
+  token<T>(s, a, row, r, lim, fixed, top, tile_log, last, last_id);
+}
+
+template <int T, bool BF16>
+__global__ __launch_bounds__(T) void draw_left_kernel(DrawArgs a, const int* left) {
+  __shared__ Shared s;
+  if (left[blockIdx.x]) left_row<T, BF16>(a, blockIdx.x, s);
+}
+
+// ---- slices ------------------------------------------------------------------------------------------
+constexpr int kSliceT = 512, kMostSlices = 8;  // threads; slices of a row
+constexpr int kWindow = 1024;                  // bins that a slice leaves: 32 below its maximum
+
+// What a slice leaves of step 1: the topmost kWindow of its bins with tokens, which reach as far down as those of the row.
+struct Slice {
+  unsigned top_key, bad;
+  double ref;
+  int high, pad;       // its topmost bin
+  u64 all;             // its tokens
+  double total;        // and their mass times exp(-ref), of 2^-f
+  struct {
+    u64 mass;
+    unsigned cnt, pad;
+  } bin[kWindow];      // bins high, high - 1, ...
+};
+// What a row's slices leave of steps 2 and 3.
+struct RowZone {
+  unsigned n;          // entries of the list; more than kList: the list is not whole
+  int law, left;
+  float top;
+  unsigned least;
+  double ref;
+  Zone z;
+  int high;            // topmost bin
+  unsigned above_k;
+  double mass[kWindow];  // above bins high, high - 1, ...
+  u64 list[kList];
+};
+struct Slices {
+  Slice* slice;     // [rows, n]
+  RowZone* row;     // [rows]
+  u64* tile;        // [rows, tiles] kept mass
+  unsigned* kept;   // [rows, n]
+  int n, log, tiles;  // slices per row, of 2^log positions; tiles per row
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(kSliceT) void draw_bins_kernel(DrawArgs a, Slices sl) {
+  constexpr int T = kSliceT;
+  __shared__ Shared s;
+  const int tid = threadIdx.x, row = blockIdx.x / sl.n, i = blockIdx.x % sl.n;
+  Row<BF16> r;
+  Limits lim;
+  set_up(a, row, r, lim);
+  set_powers(s);
+  const Fixed fixed(a.V);
+  clear<T>(s);
+  if (tid == 0 && i == 0) sl.row[row].n = 0;
+  lds_barrier();
+  const Bins bins = bins_of<T>(s, r);
+  float high = -INFINITY;
+  const int begin = i << (sl.log - 2), end = min(r.vectors(), (i + 1) << (sl.log - 2));
+  count<T>(s, r, begin, end, lim, bins, fixed, high);
+  const float top = top_of(s, high);
+  Slice& o = sl.slice[blockIdx.x];
+  const int b0 = top >= kNone ? bins.of(top) : 0;
+  if (by_k(lim) || by_p(lim)) {
+    for (int j = tid; j < kWindow; j += T) {
+      const int bin = b0 - j;
+      o.bin[j] = {by_p(lim) && bin >= 0 ? s.mass[bin] : 0, by_k(lim) && bin >= 0 ? s.cnt[bin] : 0, 0};
     }
     u64 all;
     double total;
-    u64 c_at = block_scan((u64)c, s.part, all) - c;
-    const double w_to = block_scan(w, (double*)s.part, total);
-    double w_at = w_to - w;
+    totals<T>(s, lim, bins, bins.ref, kBins, all, total);  // (at most 48 above the sample: no overflow)
     if (tid == 0) {
-      s.found[0] = 0xffffffffu;
-      s.found[1] = s.found[2] = 0xffffffffu;
+      o.all = all;
+      o.total = total;
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int bin = kBins - 1 - 4 * tid - i;
-      if (by_k && c_at < lim.k && c_at + ci[i] >= lim.k && lim.k < all) {
-        s.found[0] = bin;
-        s.value[0] = w_at;
-        s.value[1] = w_at + wi[i];
-      }
-      s.cnt[bin] = (unsigned)c_at;                          // from here on: above the bin
-      s.mass[bin] = __builtin_bit_cast(u64, w_at);
-      c_at += ci[i];
-      w_at += wi[i];
-    }
-    __syncthreads();
-    const bool ends = s.found[0] != 0xffffffffu;
-    bin_k = ends ? (int)s.found[0] : -1;
-    above_k = ends ? s.value[0] : total;
-    if (by_p) {
-      // with the mass top-k leaves somewhere in [lowest, highest], and a little room for the sums' rounding
-      const double lowest = lim.p * (ends ? s.value[0] : total) * (1 - 1e-12), highest = lim.p * (ends ? s.value[1] : total) * (1 + 1e-12);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int bin = kBins - 1 - 4 * tid - i;
-        const double before = __builtin_bit_cast(double, s.mass[bin]);
-        if (wi[i] > 0) {
-          if (before + wi[i] >= lowest) atomicMin(&s.found[1], (unsigned)(kBins - 1 - bin));  // the first bin that may reach it
-          if (before < highest) atomicMin(&s.found[2], (unsigned)bin);                        // the last one that may be needed
-        }
-      }
-      __syncthreads();
-      p_high = kBins - 1 - (int)s.found[1];
-      p_low = (int)s.found[2];
-      if (ends && p_low < bin_k) p_low = bin_k;
-      if (ends && p_high < bin_k) p_high = bin_k;
-    }
-  }
-  const int sure = max(by_p ? p_high : -1, by_p ? -1 : bin_k);  // bins above it are kept whole
-  const bool zone = by_p || bin_k >= 0;
-  auto in_k = [&](float y) { return bin_k >= 0 && bins.of(y) == bin_k; };
-  auto in_p = [&](float y) { const int bin = bins.of(y); return by_p && bin >= p_low && bin <= p_high; };
-  __syncthreads();
-
-  // 3. what is sure, and the list
-  const int tile_log = max(12, log_v - 9);
-  auto weight = [&](float y) { return (u64)(exp((double)y - (double)top) * scale + 0.5); };
-  unsigned kept_here = 0;
-  each(r, [&](int v, const float(&y)[4]) {
-    float o[4];
-    u64 w[4], sum = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool is = y[i] >= kNone;
-      const int bin = is ? bins.of(y[i]) : -1;
-      const bool keep = is && (!zone || bin > sure) && key_of(y[i]) >= lim.least;
-      o[i] = keep ? y[i] : -INFINITY;
-      w[i] = 0;
-      if (keep) {
-        w[i] = weight(y[i]);
-        ++kept_here;
-      }
-      sum += w[i];
-      if (is && zone && (bin == bin_k || (by_p && bin >= p_low && bin <= p_high))) {
-        const unsigned p = atomicAdd(&s.list_n, 1u);
-        if (p < kList) s.list[p] = ((u64)key_of(y[i]) << 32) | (unsigned)~(v + i);
-      }
-    }
-    if (__ballot(sum != 0)) {
-      const int v0 = v - 4 * (int)(threadIdx.x & 63);  // of the wavefront
-      if (v0 >= 0 && v0 >> tile_log == (v0 + 255) >> tile_log) {
-#pragma unroll
-        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-        if (v == v0) atomicAdd(&s.tile[v >> tile_log], sum);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (w[i]) atomicAdd(&s.tile[(v + i) >> tile_log], w[i]);
-      }
-    }
-    if (r.out) r.store(v, o);
-  });
-  if (kept_here) atomicAdd(&s.kept, kept_here);
-  __syncthreads();
-
-  // 4. the last token kept: key `last`, id `last_id`
-  unsigned last = 0, last_id = 0x7fffffffu;
-  if (zone) {
-    const unsigned n = s.list_n;
-    if (n <= kList) {
-      unsigned size = 2;
-      while (size < n) size <<= 1;
-      for (unsigned i = n + tid; i < size; i += T) s.list[i] = 0;
-      __syncthreads();
-      for (unsigned k = 2; k <= size; k <<= 1)
-        for (unsigned d = k >> 1; d; d >>= 1) {
-          for (unsigned i = tid; i < size / 2; i += T) {
-            const unsigned x = 2 * i - (i & (d - 1)), y = x + d;
-            const u64 p = s.list[x], q = s.list[y];
-            if ((p < q) == ((x & k) == 0)) {  // descending
-              s.list[x] = q;
-              s.list[y] = p;
-            }
-          }
-          __syncthreads();
-        }
-      // two neighbours per thread: rank, and mass before, from the sums above their bin and the list's tokens of that bin in front
-      float y[2];
-      int bin[2];
-      u64 w[2], dummy;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const unsigned p = 2 * tid + i;
-        const bool is = p < n;
-        y[i] = is ? of_key((unsigned)(s.list[p] >> 32)) : 0.f;
-        bin[i] = is ? bins.of(y[i]) : -1;
-        w[i] = is && by_p ? (u64)(bins.weight(y[i], bin[i]) * scale + 0.5) : 0;
-      }
-      u64 w_to = block_scan(w[0] + w[1], s.part, dummy);
-      const u64 w_before[2] = {w_to - w[1] - w[0], w_to - w[1]};
-      // where each token's bin begins in the list, by binary search
-      unsigned first[2];
-      u64 of_bin[2];
-      __syncthreads();
-      // sums in front of each list entry, for the entries that begin a bin
-      u64* const sums = s.mass;  // entries of bins outside of the zone are not needed any more: the zone's are read first
-      double above[2];
-      unsigned c_above[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        above[i] = bin[i] >= 0 ? __builtin_bit_cast(double, s.mass[bin[i]]) : 0;
-        c_above[i] = bin[i] >= 0 ? s.cnt[bin[i]] : 0;
-      }
-      __syncthreads();
-      sums[2 * tid] = w_before[0];
-      sums[2 * tid + 1] = w_before[1];
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        unsigned lo = 0, hi = 2 * tid + i;  // first entry of the same bin
-        if (bin[i] >= 0)
-          while (lo < hi) {
-            const unsigned mid = (lo + hi) / 2;
-            if (bins.of(of_key((unsigned)(s.list[mid] >> 32))) > bin[i]) lo = mid + 1;
-            else hi = mid;
-          }
-        first[i] = lo;
-        of_bin[i] = bin[i] >= 0 ? sums[lo] : 0;
-      }
-      // what top-k leaves
-      double target = INFINITY;
-      if (by_p) {
-        u64 mine = 0, in_bin;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (bin[i] >= 0 && bin[i] == bin_k && c_above[i] + (2 * tid + i - first[i]) < lim.k) mine += w[i];
-        block_scan(mine, s.part, in_bin);
-        target = lim.p * kReached * (above_k + (bin_k >= 0 ? (double)in_bin * exp(bins.middle(bin_k) - (double)top) : 0));
-      }
-      unsigned mine = 0;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (bin[i] < 0) continue;
-        const unsigned rank = c_above[i] + (2 * tid + i - first[i]);
-        const double before = above[i] + (double)(w_before[i] - of_bin[i]) * exp(bins.middle(bin[i]) - (double)top);
-        const unsigned key = (unsigned)(s.list[2 * tid + i] >> 32);
-        if ((bin_k < 0 || rank < lim.k) && (!by_p || before < target) && key >= lim.least) ++mine;
-      }
-      u64 kept;
-      block_scan((u64)mine, s.part, kept);
-      if (kept) {
-        const u64 e = s.list[kept - 1];
-        last = (unsigned)(e >> 32);
-        last_id = ~(unsigned)e;
-      } else {
-        last = (unsigned)(s.list[0] >> 32) + 1;
-        last_id = 0x7fffffffu;
-      }
-      for (unsigned i = tid; i < kept; i += T) {
-        const float v = of_key((unsigned)(s.list[i] >> 32));
-        const int id = (int)~(unsigned)s.list[i];
-        atomicAdd(&s.tile[id >> tile_log], weight(v));
-        if (r.out) r.out[id] = v;
-      }
-      if (tid == 0) s.kept += (unsigned)kept;
-      __syncthreads();
-    } else {
-      // top-k, then top-p, by readings
-      const double above_p = by_p ? __builtin_bit_cast(double, s.mass[p_high]) : 0;
-      const unsigned c_k = bin_k >= 0 ? s.cnt[bin_k] : 0;
-      __syncthreads();
-      unsigned ids = 0xffffffffu;  // how many tokens of key `last` are kept
-      double left = above_k;
-      if (bin_k >= 0) {
-        narrow(s, r, in_k, false, (u64)(lim.k - c_k), 0.0, top, scale, last, ids);
-        if (by_p) {
-          // mass of what top-k keeps of its bin
-          u64 mine = 0, in_bin;
-          each(r, [&](int, const float(&y)[4]) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (y[i] >= kNone && in_k(y[i]) && key_of(y[i]) > last) mine += (u64)(bins.weight(y[i], bin_k) * scale + 0.5);
-          });
-          block_scan(mine, s.part, in_bin);
-          const u64 each_w = (u64)(bins.weight(of_key(last), bin_k) * scale + 0.5);
-          left += ((double)in_bin + (double)ids * (double)each_w) * exp(bins.middle(bin_k) - (double)top);
-        }
-      }
-      if (by_p) {
-        unsigned last_p, ids_p;
-        // relative to the zone's largest token, found as the first in its order
-        unsigned high, one;
-        narrow(s, r, in_p, false, (u64)1, 0.0, top, scale, high, one);
-        const float high_y = of_key(high);
-        const double need = (lim.p * kReached * left - above_p) * exp((double)top - (double)high_y);
-        if (need > 0) narrow(s, r, in_p, true, (u64)0, need, high_y, scale, last_p, ids_p);
-        else { last_p = high; ids_p = 0; }
-        if (last_p > last || (last_p == last && ids_p < ids)) {
-          last = last_p;
-          ids = ids_p;
-        }
-      }
-      // the id of the last of them
-      __syncthreads();
-      unsigned* const per_tile = s.cnt;
-      for (int i = tid; i < kTiles; i += T) per_tile[i] = 0;
-      __syncthreads();
-      each(r, [&](int v, const float(&y)[4]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (y[i] >= kNone && key_of(y[i]) == last) atomicAdd(&per_tile[(v + i) >> tile_log], 1u);
-      });
-      __syncthreads();
-      if (tid == 0) {
-        s.found[0] = 0xffffffffu;
-        unsigned before = 0;
-        for (int i = 0; i < kTiles; ++i) {
-          if (before < ids && before + per_tile[i] >= ids) { s.found[0] = i; s.found[1] = before; }
-          before += per_tile[i];
-        }
-        s.found[2] = ids ? 0x7fffffffu : 0xffffffffu;
-      }
-      __syncthreads();
-      const unsigned in_tile = s.found[0];
-      if (in_tile != 0xffffffffu) {
-        u64 before = s.found[1];
-        __syncthreads();
-        for (int v0 = (int)in_tile << tile_log; v0 < min(a.V, (int)(in_tile + 1) << tile_log); v0 += T) {
-          const int v = v0 + tid;
-          float y = -INFINITY;
-          if (v < a.V) y = r.at(v);
-          const u64 is = y >= kNone && key_of(y) == last;
-          u64 all;
-          const u64 to = before + block_scan(is, s.part, all);
-          if (is && to == ids) s.found[2] = (unsigned)v;
-          before += all;
-        }
-        __syncthreads();
-      }
-      last_id = s.found[2];
-      // what the zone keeps
-      const int lowest = by_p ? p_low : bin_k;
-      each(r, [&](int v, const float(&y)[4]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (y[i] >= kNone) {
-            const unsigned k = key_of(y[i]);
-            const int bin = bins.of(y[i]);
-            if (bin <= sure && bin >= lowest && k >= lim.least && (k > last || (k == last && v + i <= (int)last_id))) {
-              atomicAdd(&s.tile[(v + i) >> tile_log], weight(y[i]));
-              atomicAdd(&s.kept, 1u);
-              if (r.out) r.out[v + i] = y[i];
-            }
-          }
-        }
-      });
-      __syncthreads();
-    }
-  }
-
-  // 5. the token
-  u64 mine = 0, total;
-  if (tid < kTiles) mine = s.tile[tid];
-  const u64 to = block_scan(mine, s.part, total);
-  const float u = a.uniforms ? fminf(fmaxf(a.uniforms[row], 0.f), 1.f) : 0.f;
-  const double target = (double)u * (double)total;
-  if (tid == 0) s.found[0] = 0xffffffffu;
-  __syncthreads();
-  if (mine && (double)to >= target && (double)(to - mine) < target + (target == 0 && to == mine)) s.found[0] = tid, s.sum = to - mine;
-  __syncthreads();
-  if (tid == 0) {
-    if (a.out_lse) a.out_lse[row] = (float)((double)top + log((double)total / scale));
-    if (a.out_kept) a.out_kept[row] = (int)s.kept;
-    s.found[1] = 0x7fffffffu;
-  }
-  if (!a.out_tokens && !a.out_conf) return;
-  const int tile = (int)s.found[0];
-  u64 before = s.sum;
-  __syncthreads();
-  const int end = min(a.V, (tile + 1) << tile_log);
-  for (int v0 = tile << tile_log; v0 < end; v0 += kTile) {
-    u64 w[4], sum = 0, all;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int v = v0 + 4 * tid + i;
-      w[i] = 0;
-      if (v < end) {
-        const float y = r.at(v);
-        const unsigned k = key_of(y);
-        if (y >= kNone && k >= lim.least && (k > last || (k == last && v <= (int)last_id))) w[i] = weight(y);
-      }
-      sum += w[i];
-    }
-    u64 to_here = before + block_scan(sum, s.part, all) - sum;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      to_here += w[i];
-      if (w[i] && (double)to_here >= target) atomicMin(&s.found[1], (unsigned)(v0 + 4 * tid + i));
-    }
-    before += all;
-    __syncthreads();
-    if (s.found[1] != 0x7fffffffu) break;
   }
   if (tid == 0) {
-    const int v = (int)s.found[1];
-    if (a.out_tokens) a.out_tokens[row] = v;
-    if (a.out_conf) a.out_conf[row] = (float)((double)weight(r.at(v)) / (double)total);
+    o.top_key = key_of(top);
+    o.bad = s.found[1];
+    o.ref = bins.ref;
+    o.high = b0;
   }
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(T) void draw_rows_kernel(DrawArgs a) {
+__global__ __launch_bounds__(kSliceT) void draw_keep_kernel(DrawArgs a, Slices sl) {
+  constexpr int T = kSliceT, kPer = kWindow / T;
   __shared__ Shared s;
-  draw_row<BF16>(a, blockIdx.x, s);
+  const int tid = threadIdx.x, row = blockIdx.x / sl.n, at = blockIdx.x % sl.n, n = sl.n;
+  const Slice* const slice = sl.slice + (size_t)row * n;
+  RowZone& o = sl.row[row];
+  Row<BF16> r;
+  Limits lim;
+  set_up(a, row, r, lim);
+  set_powers(s);
+  for (int i = tid; i < kTiles; i += T) s.tile[i] = 0;
+  if (tid == 0) s.found[0] = s.found[1] = s.found[3] = s.kept = s.list_n = 0;
+  const Bins bins{slice[0].ref};
+  u64 all = 0;
+  double total = 0;
+  lds_barrier();
+  if (tid < n) {
+    atomicMax(&s.found[0], slice[tid].top_key);
+    atomicMax(&s.found[3], (unsigned)slice[tid].high);
+    if (slice[tid].bad) s.found[1] = 1;
+    s.list[tid] = (u64)slice[tid].high;
+    s.list[64 + tid] = slice[tid].all;
+    s.list[128 + tid] = __builtin_bit_cast(u64, slice[tid].total);
+  }
+  lds_barrier();
+  const float top = of_key(s.found[0]);
+  const bool law = lim.law && top >= kNone && !s.found[1];
+  const int b0 = (int)s.found[3];
+  const int begin = at << (sl.log - 2), end = min(r.vectors(), (at + 1) << (sl.log - 2));
+  Zone z{-1, kBins, -1, -1, 0, 0};
+  bool here = true;
+  if (law) {
+    set_least(lim, top);
+    if (by_k(lim) || by_p(lim)) {
+      for (int i = 0; i < n; ++i) {
+        all += s.list[64 + i];
+        total += __builtin_bit_cast(double, s.list[128 + i]);
+      }
+      total *= exp(bins.ref - (double)top);
+      unsigned c[kPer] = {};
+      u64 w[kPer] = {};
+      {
+        unsigned ci[kMostSlices][kPer];
+        u64 wi[kMostSlices][kPer];
+#pragma unroll
+        for (int i = 0; i < kMostSlices; ++i)
+#pragma unroll
+          for (int q = 0; q < kPer; ++q) {
+            const int k = min(i, n - 1), j = (int)s.list[k] - (b0 - kPer * tid - q);
+            const bool is = i < n && j >= 0;
+            ci[i][q] = is ? slice[k].bin[j].cnt : 0;
+            wi[i][q] = is ? slice[k].bin[j].mass : 0;
+          }
+#pragma unroll
+        for (int i = 0; i < kMostSlices; ++i)
+#pragma unroll
+          for (int q = 0; q < kPer; ++q) {
+            c[q] += ci[i][q];
+            w[q] += wi[i][q];
+          }
+      }
+#pragma unroll
+      for (int q = 0; q < kPer; ++q) {
+        const int bin = b0 - kPer * tid - q;
+        if (bin >= 0) {
+          s.cnt[bin] = c[q];
+          s.mass[bin] = w[q];
+        }
+      }
+      lds_barrier();
+      here = find_zone<T, kPer, false, false>(s, lim, bins, top, b0, all, total, z) && bins.serve(top);
+      lds_barrier();
+    }
+  }
+  if (at == 0) {
+    if (tid == 0) {
+      o.law = law;
+      o.left = !here;
+      o.top = top;
+      o.ref = bins.ref;
+      o.least = lim.least;
+      o.high = b0;
+      o.above_k = s.above_k;
+      o.z = z;
+    }
+    if (z.zone && by_p(lim))
+#pragma unroll
+      for (int q = 0; q < kPer; ++q) o.mass[kPer * tid + q] = b0 >= kPer * tid + q ? __builtin_bit_cast(double, s.mass[b0 - kPer * tid - q]) : 0;
+  }
+  if (!law) no_logits<T>(r, begin, end);
+  if (!law || !here) return;
+  const int tile_log = tile_log_of(a.V);
+  const unsigned kept = keep<T>(s, r, begin, end, lim, bins, Fixed(a.V), z, top, tile_log);
+  if (kept) atomicAdd(&s.kept, kept);
+  lds_barrier();
+  const unsigned mine = s.list_n;
+  if (tid == 0 && mine) s.found[2] = atomicAdd(&o.n, mine);
+  lds_barrier();
+  for (unsigned i = tid; i < min(mine, (unsigned)kList); i += T)
+    if (s.found[2] + i < kList) o.list[s.found[2] + i] = s.list[i];
+  const int t0 = at << (sl.log - tile_log), t1 = min(sl.tiles, (at + 1) << (sl.log - tile_log));
+  for (int t = t0 + tid; t < t1; t += T) sl.tile[(size_t)row * sl.tiles + t] = s.tile[t];
+  if (tid == 0) sl.kept[blockIdx.x] = s.kept;
 }
+
+template <bool BF16>
+__global__ __launch_bounds__(kSliceT) void draw_finish_kernel(DrawArgs a, Slices sl) {
+  constexpr int T = kSliceT;
+  __shared__ Shared s;
+  const int tid = threadIdx.x, row = blockIdx.x;
+  const RowZone& o = sl.row[row];
+  Row<BF16> r;
+  Limits lim;
+  set_up(a, row, r, lim);
+  set_powers(s);
+  if (tid == 0) s.kept = 0;
+  const unsigned n = o.n;
+  if (!o.law) {
+    no_token(a, row);
+    return;
+  }
+  if (o.left || n > kList) {
+    left_row<T, BF16>(a, row, s);
+    return;
+  }
+  const Zone z = o.z;
+  const float top = o.top;
+  const Bins bins{o.ref};
+  lim.least = o.least;
+  for (int j = tid; j < kTiles; j += T) s.tile[j] = j < sl.tiles ? sl.tile[(size_t)row * sl.tiles + j] : 0;
+  for (unsigned j = tid; j < n; j += T) s.list[j] = o.list[j];
+  if (by_p(lim))
+    for (int j = tid; j < kWindow; j += T)
+      if (o.high >= j) s.mass[o.high - j] = __builtin_bit_cast(u64, o.mass[j]);
+  if (tid == 0) s.above_k = o.above_k;
+  lds_barrier();
+  if (tid < sl.n) atomicAdd(&s.kept, sl.kept[(size_t)row * sl.n + tid]);
+  lds_barrier();
+  const Fixed fixed(a.V);
+  const int tile_log = tile_log_of(a.V);
+  unsigned last = 0;
+  int last_id = 0x7fffffff;
+  if (z.zone) resolve<T>(s, r, lim, bins, fixed, z, top, tile_log, n, last, last_id);
+  token<T>(s, a, row, r, lim, fixed, top, tile_log, last, last_id);
+}
+
+// Slices of a call: 0, or their number for each row, of 2^*log positions each.
+int slices_of(int rows, int V, int* log) {
+  *log = 12 > tile_log_of(V) ? 12 : tile_log_of(V);
+  if (rows >= kManyRows || V < kShort) return 0;
+  while (((long)V + 3 + (1L << *log) - 1) >> *log > kMostSlices) ++*log;
+  return (int)(((long)V + 3 + (1L << *log) - 1) >> *log);
+}
+int tiles_of(int V) { return (int)(((long)V + 3 + (1L << tile_log_of(V)) - 1) >> tile_log_of(V)); }
 
 }  // namespace
 
-size_t draw_workspace(int, int) { return 256; }
+size_t draw_workspace(int rows, int V) {
+  int log;
+  const size_t n = (size_t)slices_of(rows, V, &log) * rows;
+  return n ? n * (sizeof(Slice) + sizeof(unsigned)) + rows * (sizeof(RowZone) + tiles_of(V) * sizeof(u64)) : (size_t)rows * sizeof(int);
+}
 
 hipError_t launch_draw(const DrawArgs& a) {
-  const dim3 grid(a.B * a.K), threads(T);
-  if (a.bf16) hipLaunchKernelGGL(draw_rows_kernel<true>, grid, threads, 0, a.stream, a);
-  else hipLaunchKernelGGL(draw_rows_kernel<false>, grid, threads, 0, a.stream, a);
+  const int rows = a.B * a.K;
+  Slices sl;
+  sl.n = slices_of(rows, a.V, &sl.log);
+  sl.tiles = tiles_of(a.V);
+  const size_t n = (size_t)sl.n * rows;
+  sl.slice = (Slice*)a.workspace;
+  sl.row = (RowZone*)(sl.slice + n);
+  sl.tile = (u64*)(sl.row + rows);
+  sl.kept = (unsigned*)(sl.tile + (size_t)rows * sl.tiles);
+  int* const left = (int*)a.workspace;
+  auto run = [&](auto bf16) {
+    constexpr bool B16 = decltype(bf16)::value;
+    if (n) {
+      hipLaunchKernelGGL(draw_bins_kernel<B16>, dim3((unsigned)n), dim3(kSliceT), 0, a.stream, a, sl);
+      hipLaunchKernelGGL(draw_keep_kernel<B16>, dim3((unsigned)n), dim3(kSliceT), 0, a.stream, a, sl);
+      hipLaunchKernelGGL(draw_finish_kernel<B16>, dim3(rows), dim3(kSliceT), 0, a.stream, a, sl);
+    } else if (a.V < kShort) {
+      hipLaunchKernelGGL((draw_rows_kernel<512, B16, true>), dim3(rows), dim3(512), 0, a.stream, a, left);
+    } else {
+      hipLaunchKernelGGL((draw_rows_kernel<512, B16, false>), dim3(rows), dim3(512), 0, a.stream, a, left);
+      hipLaunchKernelGGL((draw_left_kernel<512, B16>), dim3(rows), dim3(512), 0, a.stream, a, left);
+    }
+  };
+  if (a.bf16) run(std::true_type{});
+  else run(std::false_type{});
   return hipGetLastError();
 }
 
