@@ -15,8 +15,6 @@ namespace {
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
-constexpr float kLog2e = 1.4426950408889634f;
-
 // ---------------------------------------------------------------------------------------------
 // G from z
 // ---------------------------------------------------------------------------------------------
@@ -105,7 +103,7 @@ __global__ __launch_bounds__(NT) void grad_rows_kernel(GradArgs a) {
 // ---------------------------------------------------------------------------------------------
 constexpr int kThreads = 512, BN = 256, BK = 64, WM = 2, WN = 4;
 
-// Rows of 64 k and `cols` columns in LDS, 32 bytes (16 columns) at chunk c ^ turn(k): the 32 lanes of half a transposed read, which take
+// Rows of `cols` columns in LDS, a row per k, 32 bytes (16 columns) at chunk c ^ turn(k): the 32 lanes of half a transposed read, which take
 // 32 bytes of rows 8 g + {0, 1, 2, 3} of two lane groups g, fall on different banks.
 template <int COLS>
 __device__ __forceinline__ int turn(int k) {
@@ -121,13 +119,21 @@ __device__ __forceinline__ bf16x4 read_turned(const char* p) {
 __device__ __forceinline__ bf16x8 both(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
 // AT: A is [K][M] (m contiguous), else [M][K].  OUT: __bf16 for C itself, float for the partial sums of a share of k.
+//
+// k goes in halves of 32 columns.  While a half is multiplied out of registers, the fragments of the next one are read from LDS, each into
+// the registers of one that has had its last use, and the halves behind that are on their way from memory to LDS: B in a ring of halves, A
+// likewise (AT), or in a ring of stages of 64 columns (rows of 128 bytes: 64-byte pieces move at 60 % of the rate out of L2).  One
+// barrier per half.
 template <int NR, bool AT, class OUT>
 __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
-  constexpr int BM = 16 * NR * WM;
-  constexpr int RA = 2, RB = 3;  // stages in LDS: A one step ahead, B two
-  constexpr int kStageA = BM * BK * 2, kStageB = BN * BK * 2;
+  constexpr int BM = 16 * NR * WM, HK = 32;
+  constexpr int RA = AT ? 5 : NR == 8 ? 3 : 4, RB = AT ? 5 : NR == 8 ? 4 : 6;
+  static_assert(AT ? RA == RB : RB % 2 == 0 && RB <= 2 * RA - 1, "the waits count on B being the younger one");
+  constexpr int kStageA = BM * (AT ? HK : BK) * 2, kStageB = BN * HK * 2;
   constexpr int kLoadsA = kStageA / 1024, LA = (kLoadsA + 7) / 8, LB = kStageB / 1024 / 8;
-  static_assert(kLoadsA >= LA && LA <= 4 && LB == 4, "");
+  static_assert(kLoadsA >= LA && LA <= 4 && LB == 2, "");
+  // loads younger than those that a half waits for
+  constexpr int kYounger = AT ? (RB - 2) * (LA + LB) : (RB - 2) * LB + (RB - 2) / 2 * LA;
   constexpr int kPitch = BN + 8;  // of the tile in LDS on its way out
   constexpr int kOut = sizeof(OUT) == 2 ? BM * kPitch * 2 : 0;
   constexpr int kRings = RA * kStageA + RB * kStageB;
@@ -147,12 +153,12 @@ __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
   const int share = (int)(id / ((long)mt * nt)), at = (int)(id % ((long)mt * nt));
   const int m0 = (a.n_first ? at / nt : at % mt) * BM, n0 = (a.n_first ? at % nt : at / mt) * BN;
   const int nk_all = a.K / BK;
-  const int k0 = (int)((long)share * nk_all / a.shares), nk = (int)((long)(share + 1) * nk_all / a.shares) - k0;
+  const int k0 = (int)((long)share * nk_all / a.shares), nk = (int)((long)(share + 1) * nk_all / a.shares) - k0, nh = 2 * nk;
 
   // Direct-to-LDS loads of 1 KB: lane l fills slot (instruction, l) of 16 bytes.
   const __bf16* ga[LA];
   const __bf16* gb[LB];
-  const int ia0 = min(wave * LA, kLoadsA - LA);
+  const int ia0 = min(wave * LA, kLoadsA - LA);  // where the rows do not divide, the last wavefronts repeat some
 #pragma unroll
   for (int q = 0; q < LA; ++q) {
     const int s = (ia0 + q) * 64 + lane;
@@ -165,29 +171,46 @@ __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
       ga[q] = a.A + (size_t)min(m0 + m, a.M - 1) * a.lda + k0 * BK + c * 8 - q * 512;
     }
   }
-  int b_row[LB];
+  int b_in[LB], b_end = k0 * BK;  // row of a load within its half; end of the half that is loaded next
 #pragma unroll
   for (int q = 0; q < LB; ++q) {
     const int s = (wave * LB + q) * 64 + lane;
     const int k = s / (BN / 8), p = s % (BN / 8);
     const int n = n0 + (((p >> 1) ^ turn<BN>(k)) * 16 + (p & 1) * 8);
-    b_row[q] = k0 * BK + k;
-    gb[q] = a.B + min(n, a.N - 8) - q * 512;
+    b_in[q] = k;
+    gb[q] = a.B + (size_t)(k0 * BK + k) * a.ldb + min(n, a.N - 8) - q * 512;
   }
   const uint32_t slotA = lds_offset(ringA) + ia0 * 1024, slotB = lds_offset(ringB) + wave * LB * 1024;
-  auto load_a = [&](int stage) __attribute__((always_inline)) {
-    load_group_to_lds<false>(ga, __builtin_amdgcn_readfirstlane(slotA + stage * kStageA));
+  int put_a = 0, put_b = 0;  // ring positions of the next loads
+  auto load_a = [&]() __attribute__((always_inline)) {
+    load_group_to_lds<false>(ga, __builtin_amdgcn_readfirstlane(slotA + put_a * kStageA));
 #pragma unroll
-    for (int q = 0; q < LA; ++q) ga[q] += AT ? (long)BK * a.lda : (long)BK;
+    for (int q = 0; q < LA; ++q) ga[q] += AT ? (long)HK * a.lda : (long)BK;
+    put_a = put_a == RA - 1 ? 0 : put_a + 1;
   };
-  auto load_b = [&](int stage) __attribute__((always_inline)) {
-    const __bf16* p[LB];
+  auto load_b = [&]() __attribute__((always_inline)) {
+    const uint32_t lds_off = __builtin_amdgcn_readfirstlane(slotB + put_b * kStageB);
+    b_end += HK;
+    if (b_end <= a.b_rows) {
+      load_group_to_lds<false>(gb, lds_off);
+    } else {  // rows past the last: the last once more, which meets zeros of A
+      const __bf16* p[LB];
 #pragma unroll
-    for (int q = 0; q < LB; ++q) {
-      p[q] = gb[q] + (size_t)min(b_row[q], a.b_rows - 1) * a.ldb;  // rows past the last meet zeros of A
-      b_row[q] += BK;
+      for (int q = 0; q < LB; ++q) p[q] = gb[q] - (long)max(0, b_end - HK + b_in[q] - (a.b_rows - 1)) * a.ldb;
+      load_group_to_lds<false>(p, lds_off);
     }
-    load_group_to_lds<false>(p, __builtin_amdgcn_readfirstlane(slotB + stage * kStageB));
+#pragma unroll
+    for (int q = 0; q < LB; ++q) gb[q] += HK * a.ldb;
+    put_b = put_b == RB - 1 ? 0 : put_b + 1;
+  };
+  // What half h brings on its way, in this order: A of half h + RB, or of stage (h - 1) / 2 + RA where h is odd; B of half h + RB.
+  auto load = [&](int h, bool odd) __attribute__((always_inline)) {
+    if constexpr (AT) {
+      if (h + RB < nh) load_a();
+    } else {
+      if (odd && (h - 1) / 2 + RA < nk) load_a();
+    }
+    if (h + RB >= 0 && h + RB < nh) load_b();
   };
 
   floatx4 acc[NR][4];
@@ -196,7 +219,7 @@ __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) acc[n][t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  // byte offsets of a lane's fragments in a stage
+  // byte offsets of a lane's fragments in a half, or stage
   const int kr = 8 * g + (i16 >> 2), cc = (i16 & 3) * 8;
   int ob[4], oa[AT ? NR : 2];
 #pragma unroll
@@ -209,37 +232,51 @@ __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
     for (int ks = 0; ks < 2; ++ks) oa[ks] = (wm * NR * 16 + i16) * 128 + (((ks * 4 + g) ^ ((i16 >> 1) & 7)) * 16);
   }
 
-  if (nk > 0) {
-    load_b(0);
-    load_a(0);
-    if (nk > 1) load_b(1);
-  }
-  int sb = 0;
-  for (int k = 0; k < nk; ++k) {
-    if (k + 1 < nk) wait_newer<LB>();  // B(k + 1) may stay on its way
-    else wait_newer<0>();
-    lds_barrier();
-    if (k + 1 < nk) load_a((k + 1) & 1);
-    if (k + 2 < nk) load_b(sb == 0 ? RB - 1 : sb - 1);
-    const char* sA = ringA + (k & 1) * kStageA;
-    const char* sB = ringB + sb * kStageB;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      bf16x8 nf[4], mf[NR];
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        nf[t] = both(read_turned(sB + ob[t] + ks * 32 * BN * 2), read_turned(sB + ob[t] + (ks * 32 + 4) * BN * 2));
-#pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        if constexpr (AT) mf[n] = both(read_turned(sA + oa[n] + ks * 32 * BM * 2), read_turned(sA + oa[n] + (ks * 32 + 4) * BM * 2));
-        else mf[n] = *reinterpret_cast<const bf16x8*>(sA + oa[ks] + n * 2048);
-      }
-#pragma unroll
-      for (int n = 0; n < NR; ++n)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf[t], mf[n], acc[n][t], 0, 0, 0);
+  bf16x8 nf[2][4], mf[NR];
+  int get_a = 0, get_b = 0;  // ring positions of the half that is read next
+  // Half h (ODD) is multiplied, half h + 1 is read.
+  auto half = [&](int h, auto odd_tag, auto mul_tag, auto read_tag) __attribute__((always_inline)) {
+    constexpr bool ODD = decltype(odd_tag)::value, MUL = decltype(mul_tag)::value, READ = decltype(read_tag)::value;
+    constexpr int cur = ODD ? 1 : 0, next = cur ^ 1;
+    if constexpr (READ) {
+      if (h + (AT ? RB - 1 : 2 * RA - 2 > RB - 1 ? 2 * RA - 2 : RB - 1) < nh) wait_newer<kYounger>();  // all of these exist
+      else wait_newer<0>();
     }
-    sb = sb == RB - 1 ? 0 : sb + 1;
+    lds_barrier();
+    load(h, ODD);
+    __builtin_amdgcn_sched_barrier(0);
+    const char* sA = ringA + get_a * kStageA;
+    const char* sB = ringB + get_b * kStageB;
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      if constexpr (MUL)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf[cur][t], mf[n], acc[n][t], 0, 0, 0);
+      if constexpr (READ) {
+#pragma unroll
+        for (int t = n * 4 / (NR < 4 ? NR : 4); t < (n + 1) * 4 / (NR < 4 ? NR : 4) && t < 4; ++t)
+          nf[next][t] = both(read_turned(sB + ob[t]), read_turned(sB + ob[t] + 4 * BN * 2));
+        if constexpr (AT) mf[n] = both(read_turned(sA + oa[n]), read_turned(sA + oa[n] + 4 * BM * 2));
+        else mf[n] = *reinterpret_cast<const bf16x8*>(sA + oa[ODD ? 0 : 1] + n * 2048);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (READ) {
+      get_b = get_b == RB - 1 ? 0 : get_b + 1;
+      if (AT || !ODD) get_a = get_a == RA - 1 ? 0 : get_a + 1;  // (the stage of the half read behind an odd one is read on)
+    }
+  };
+  using Yes = std::true_type;
+  using No = std::false_type;
+  if (nk > 0) {
+    for (int h = AT ? -RB : -2 * RA; h < -1; ++h) load(h, h & 1);
+    half(-1, Yes{}, No{}, Yes{});
+    for (int p = 0; p < nk - 1; ++p) {
+      half(2 * p, No{}, Yes{}, Yes{});
+      half(2 * p + 1, Yes{}, Yes{}, Yes{});
+    }
+    half(nh - 2, No{}, Yes{}, Yes{});
+    half(nh - 1, Yes{}, Yes{}, No{});
   }
   // acc[n][t]: columns 16 t + 4 g .. + 3 of row 16 n + i16 of the wavefront's tile
   if constexpr (sizeof(OUT) == 4) {
