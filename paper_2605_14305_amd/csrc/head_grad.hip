@@ -101,12 +101,12 @@ __global__ __launch_bounds__(NT) void grad_rows_kernel(GradArgs a) {
 // ---------------------------------------------------------------------------------------------
 // C = A B, bf16 operands
 // ---------------------------------------------------------------------------------------------
-constexpr int kThreads = 512, BN = 256, BK = 64, WM = 2, WN = 4;
+constexpr int BN = 256, BK = 64, HK = 32, WM = 2;
 
-// Rows of `cols` columns in LDS, a row per k, 32 bytes (16 columns) at chunk c ^ turn(k): the 32 lanes of half a transposed read, which take
+// Rows of `cols` columns in LDS, a row per k, 32 bytes (16 columns) at chunk c ^ turn_of(k): the 32 lanes of half a transposed read, which take
 // 32 bytes of rows 8 g + {0, 1, 2, 3} of two lane groups g, fall on different banks.
 template <int COLS>
-__device__ __forceinline__ int turn(int k) {
+__device__ __forceinline__ int turn_of(int k) {
   if constexpr (COLS >= 128) return (k & 3) | ((k >> 3) & 1) << 2;
   else return ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
 }
@@ -118,23 +118,32 @@ __device__ __forceinline__ bf16x4 read_turned(const char* p) {
 }
 __device__ __forceinline__ bf16x8 both(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// AT: A is [K][M] (m contiguous), else [M][K].  OUT: __bf16 for C itself, float for the partial sums of a share of k.
+// Tile of 32 NR rows x 256 columns, 2 x WN wavefronts of 16 NR rows.  AT: A is [K][M] (m contiguous), else [M][K].  OUT: __bf16 for C itself,
+// float for the partial sums of a share of k.
 //
-// k goes in halves of 32 columns.  While a half is multiplied out of registers, the fragments of the next one are read from LDS, each into
-// the registers of one that has had its last use, and the halves behind that are on their way from memory to LDS: B in a ring of halves, A
-// likewise (AT), or in a ring of stages of 64 columns (rows of 128 bytes: 64-byte pieces move at 60 % of the rate out of L2).  One
-// barrier per half.
-template <int NR, bool AT, class OUT>
-__global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
-  constexpr int BM = 16 * NR * WM, HK = 32;
-  constexpr int RA = AT ? 5 : NR == 8 ? 3 : 4, RB = AT ? 5 : NR == 8 ? 4 : 6;
-  static_assert(AT ? RA == RB : RB % 2 == 0 && RB <= 2 * RA - 1, "the waits count on B being the younger one");
+// k goes in halves of 32 columns.  While a half is multiplied out of registers, the fragments of the next one are read from LDS, and the
+// halves behind that are on their way from memory to LDS: B in a ring of halves, A likewise (AT), or in a ring of stages of 64 columns (rows
+// of 128 bytes: 64-byte pieces move at 60 % of the rate out of L2).  One barrier per half.
+//
+// What bounds it: LDS and the matrix units alike.  A half of 256 x 256 x 32 takes 1024 cycles of multiplies, and with eight wavefronts of
+// 128 x 64 96 KB of fragments and 32 KB on their way in, 1024 cycles of LDS.  Four wavefronts of 128 x 128 read 64 KB, but with one wavefront per
+// SIMD every other instruction holds the multiplies: grad_h of 2048 rows of d = 4096, V = 126464 1655 -> 1931 us, grad_w 1963 -> 2092.
+//   grad_h (WN = 4): few long tiles.  1655 us = 1.28 PFLOP/s (fragments read where they are multiplied, one step ahead: 1816).
+//   grad_w (WN = 2, 128 x 256): K is the number of rows, so a tile is short, and filling the rings and writing 64 KB weigh as much as the
+//     multiplies.  Two workgroups per CU, in 72 KB each, work under each other's ends: 1903 us = 1.11 PFLOP/s, against 1963 with one of
+//     256 x 256; 48 rows 290 -> 273 (3.8 TB/s written), 333 rows of d = 2048, V = 50257 128 -> 112.
+template <int NR, int WN, bool AT, class OUT>
+__global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel(ProductArgs a) {
+  constexpr int BM = 16 * NR * WM, kWaves = WM * WN, kThreads = kWave * kWaves, kColumns = BN / WN / 16;
+  constexpr int RA = WN == 2 ? 3 : NR == 8 ? 3 : 4, RB = WN == 2 ? 3 : NR == 8 ? 4 : 6;
+  static_assert(AT == (WN == 2) && (AT ? RA == RB : RB % 2 == 0 && RB <= 2 * RA - 1), "the waits count on B being the younger one");
+  constexpr bool ROLL = WN == 4;  // a fragment of A goes into the registers of the one that has had its last use, else into a second set
   constexpr int kStageA = BM * (AT ? HK : BK) * 2, kStageB = BN * HK * 2;
-  constexpr int kLoadsA = kStageA / 1024, LA = (kLoadsA + 7) / 8, LB = kStageB / 1024 / 8;
-  static_assert(kLoadsA >= LA && LA <= 4 && LB == 2, "");
+  constexpr int kLoadsA = kStageA / 1024, LA = (kLoadsA + kWaves - 1) / kWaves, LB = kStageB / 1024 / kWaves;
+  static_assert(kLoadsA >= LA && LA <= 4 && LB <= 4, "");
   // loads younger than those that a half waits for
   constexpr int kYounger = AT ? (RB - 2) * (LA + LB) : (RB - 2) * LB + (RB - 2) / 2 * LA;
-  constexpr int kPitch = BN + 8;  // of the tile in LDS on its way out
+  constexpr int kPitch = BN + 8;  // of the tile in LDS on its way out: a wavefront stores whole rows of 512 bytes
   constexpr int kOut = sizeof(OUT) == 2 ? BM * kPitch * 2 : 0;
   constexpr int kRings = RA * kStageA + RB * kStageB;
   __shared__ __align__(16) char lds[kRings > kOut ? kRings : kOut];
@@ -164,7 +173,7 @@ __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
     const int s = (ia0 + q) * 64 + lane;
     if constexpr (AT) {
       const int k = s / (BM / 8), p = s % (BM / 8);
-      const int m = m0 + (((p >> 1) ^ turn<BM>(k)) * 16 + (p & 1) * 8);
+      const int m = m0 + (((p >> 1) ^ turn_of<BM>(k)) * 16 + (p & 1) * 8);
       ga[q] = a.A + (size_t)(k0 * BK + k) * a.lda + min(m, (a.M - 1) & ~7) - q * 512;
     } else {
       const int m = s / 8, c = (s & 7) ^ ((m >> 1) & 7);
@@ -176,7 +185,7 @@ __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
   for (int q = 0; q < LB; ++q) {
     const int s = (wave * LB + q) * 64 + lane;
     const int k = s / (BN / 8), p = s % (BN / 8);
-    const int n = n0 + (((p >> 1) ^ turn<BN>(k)) * 16 + (p & 1) * 8);
+    const int n = n0 + (((p >> 1) ^ turn_of<BN>(k)) * 16 + (p & 1) * 8);
     b_in[q] = k;
     gb[q] = a.B + (size_t)(k0 * BK + k) * a.ldb + min(n, a.N - 8) - q * 512;
   }
@@ -213,26 +222,26 @@ __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
     if (h + RB >= 0 && h + RB < nh) load_b();
   };
 
-  floatx4 acc[NR][4];
+  floatx4 acc[NR][kColumns];
 #pragma unroll
   for (int n = 0; n < NR; ++n)
 #pragma unroll
-    for (int t = 0; t < 4; ++t) acc[n][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < kColumns; ++t) acc[n][t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
   // byte offsets of a lane's fragments in a half, or stage
   const int kr = 8 * g + (i16 >> 2), cc = (i16 & 3) * 8;
-  int ob[4], oa[AT ? NR : 2];
+  int ob[kColumns], oa[AT ? NR : 2];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) ob[t] = kr * (BN * 2) + ((wn * 4 + t) ^ turn<BN>(kr)) * 32 + cc;
+  for (int t = 0; t < kColumns; ++t) ob[t] = kr * (BN * 2) + ((wn * kColumns + t) ^ turn_of<BN>(kr)) * 32 + cc;
   if constexpr (AT) {
 #pragma unroll
-    for (int n = 0; n < NR; ++n) oa[n] = kr * (BM * 2) + ((wm * NR + n) ^ turn<BM>(kr)) * 32 + cc;
+    for (int n = 0; n < NR; ++n) oa[n] = kr * (BM * 2) + ((wm * NR + n) ^ turn_of<BM>(kr)) * 32 + cc;
   } else {
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) oa[ks] = (wm * NR * 16 + i16) * 128 + (((ks * 4 + g) ^ ((i16 >> 1) & 7)) * 16);
   }
 
-  bf16x8 nf[2][4], mf[NR];
+  bf16x8 nf[2][kColumns], mf[ROLL ? 1 : 2][NR];
   int get_a = 0, get_b = 0;  // ring positions of the half that is read next
   // Half h (ODD) is multiplied, half h + 1 is read.
   auto half = [&](int h, auto odd_tag, auto mul_tag, auto read_tag) __attribute__((always_inline)) {
@@ -247,20 +256,37 @@ __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
     __builtin_amdgcn_sched_barrier(0);
     const char* sA = ringA + get_a * kStageA;
     const char* sB = ringB + get_b * kStageB;
+    auto read_n = [&](int t) __attribute__((always_inline)) {
+      nf[next][t] = both(read_turned(sB + ob[t]), read_turned(sB + ob[t] + 4 * BN * 2));
+    };
+    auto read_m = [&](int n) __attribute__((always_inline)) {
+      bf16x8& f = mf[ROLL ? 0 : next][n];
+      if constexpr (AT) f = both(read_turned(sA + oa[n]), read_turned(sA + oa[n] + 4 * BM * 2));
+      else f = *reinterpret_cast<const bf16x8*>(sA + oa[ODD ? 0 : 1] + n * 2048);
+    };
+    // ROLL: behind a row's multiplies, its own and some of the columns' fragments; else one behind every second multiply or so
+    constexpr int kReads = NR + kColumns, kEvery = NR * kColumns * 3 / 4 / kReads < 1 ? 1 : NR * kColumns * 3 / 4 / kReads;
+    static_assert(ROLL || kReads * kEvery <= NR * kColumns, "");
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      if constexpr (MUL)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf[cur][t], mf[n], acc[n][t], 0, 0, 0);
-      if constexpr (READ) {
-#pragma unroll
-        for (int t = n * 4 / (NR < 4 ? NR : 4); t < (n + 1) * 4 / (NR < 4 ? NR : 4) && t < 4; ++t)
-          nf[next][t] = both(read_turned(sB + ob[t]), read_turned(sB + ob[t] + 4 * BN * 2));
-        if constexpr (AT) mf[n] = both(read_turned(sA + oa[n]), read_turned(sA + oa[n] + 4 * BM * 2));
-        else mf[n] = *reinterpret_cast<const bf16x8*>(sA + oa[ODD ? 0 : 1] + n * 2048);
+    for (int x = 0; x < NR * kColumns; ++x) {
+      const int n = x / kColumns, t = x % kColumns;
+      if constexpr (MUL) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nf[cur][t], mf[ROLL ? 0 : cur][n], acc[n][t], 0, 0, 0);
+      if constexpr (READ && ROLL) {
+        if (t == kColumns - 1) {
+          constexpr int kRows = NR < kColumns ? NR : kColumns;
+          for (int q = n * kColumns / kRows; q < (n + 1) * kColumns / kRows && q < kColumns; ++q) read_n(q);
+          read_m(n);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else if constexpr (READ) {
+        if (x % kEvery == 0 && x / kEvery < kReads) {
+          if (x / kEvery < kColumns) read_n(x / kEvery);
+          else read_m(x / kEvery - kColumns);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_sched_barrier(0);
     if constexpr (READ) {
       get_b = get_b == RB - 1 ? 0 : get_b + 1;
       if (AT || !ODD) get_a = get_a == RA - 1 ? 0 : get_a + 1;  // (the stage of the half read behind an odd one is read on)
@@ -285,8 +311,8 @@ __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
     for (int n = 0; n < NR; ++n) {
       const int m = m0 + (wm * NR + n) * 16 + i16;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int c = n0 + (wn * 4 + t) * 16 + 4 * g;
+      for (int t = 0; t < kColumns; ++t) {
+        const int c = n0 + (wn * kColumns + t) * 16 + 4 * g;
         if (m < a.M && c < a.N) {
           floatx4* p = reinterpret_cast<floatx4*>(C + (size_t)m * a.N + c);
           *p = a.add ? *p + acc[n][t] : acc[n][t];
@@ -299,11 +325,11 @@ __global__ __launch_bounds__(kThreads) void grad_product_kernel(ProductArgs a) {
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
+      for (int t = 0; t < kColumns; ++t) {
         bf16x4 o;
 #pragma unroll
         for (int c = 0; c < 4; ++c) o[c] = (__bf16)acc[n][t][c];
-        *reinterpret_cast<bf16x4*>(tile + ((wm * NR + n) * 16 + i16) * kPitch + (wn * 4 + t) * 16 + 4 * g) = o;
+        *reinterpret_cast<bf16x4*>(tile + ((wm * NR + n) * 16 + i16) * kPitch + (wn * kColumns + t) * 16 + 4 * g) = o;
       }
     lds_barrier();
     __bf16* C = (__bf16*)a.C;
@@ -327,13 +353,14 @@ __global__ __launch_bounds__(256) void grad_sum_kernel(const float* part, int sh
     if (i + c < n) out[i + c] = (OUT)s[c];
 }
 
-template <int NR, bool AT>
+template <int NR, int WN, bool AT>
 hipError_t launch_rows(const ProductArgs& a, bool partial, hipStream_t stream) {
   constexpr int BM = 16 * NR * WM;
   const long tiles = (long)((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN) * a.shares;
-  const dim3 grid((unsigned)(8 * ((tiles + 7) / 8))), threads(kThreads);
-  if (partial) hipLaunchKernelGGL((grad_product_kernel<NR, AT, float>), grid, threads, 0, stream, a);
-  else hipLaunchKernelGGL((grad_product_kernel<NR, AT, __bf16>), grid, threads, 0, stream, a);
+  if (tiles >= 1L << 23) return hipErrorInvalidValue;  // 2^32 threads
+  const dim3 grid((unsigned)(8 * ((tiles + 7) / 8))), threads(128 * WN);
+  if (partial) hipLaunchKernelGGL((grad_product_kernel<NR, WN, AT, float>), grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL((grad_product_kernel<NR, WN, AT, __bf16>), grid, threads, 0, stream, a);
   return hipGetLastError();
 }
 
@@ -365,12 +392,12 @@ int grad_h_shares(int rows, int d, int V) {
 hipError_t launch_grad_h(const ProductArgs& a, hipStream_t stream) {
   const bool partial = a.shares > 1;
   switch (grad_h_rows(a.M)) {
-    case 32: return launch_rows<1, false>(a, partial, stream);
-    case 64: return launch_rows<2, false>(a, partial, stream);
-    case 128: return launch_rows<4, false>(a, partial, stream);
-    default: return launch_rows<8, false>(a, partial, stream);
+    case 32: return launch_rows<1, 4, false>(a, partial, stream);
+    case 64: return launch_rows<2, 4, false>(a, partial, stream);
+    case 128: return launch_rows<4, 4, false>(a, partial, stream);
+    default: return launch_rows<8, 4, false>(a, partial, stream);
   }
 }
-hipError_t launch_grad_w(const ProductArgs& a, bool partial, hipStream_t stream) { return launch_rows<8, true>(a, partial, stream); }
+hipError_t launch_grad_w(const ProductArgs& a, bool partial, hipStream_t stream) { return launch_rows<4, 2, true>(a, partial, stream); }
 
 }  // namespace fef
