@@ -635,14 +635,14 @@ fef_status grad_layout(const fef_params* p, int32_t R, GradLayout* L) {
   if (p->ev_head_begin || p->ev_head_end) return fail(FEF_ERR_INVALID_ARG, "ev_head_begin and ev_head_end must be NULL in this call");
   L->rows = R < kGradRows ? R : kGradRows;
   L->blocks = (R + kGradRows - 1) / kGradRows;
-  L->padded = bf16 ? (int)align_up((size_t)L->rows, 64) : L->rows;
+  L->padded = (int)align_up((size_t)L->rows, 64);
   L->ldl = (long)align_up((size_t)p->V, 64);
   L->nT = bf16 ? (p->V + fef::kTiled256Tn - 1) / fef::kTiled256Tn : (p->V + fef::kTiledTn - 1) / fef::kTiledTn;
   const size_t e = bf16 ? 2 : 4, d = (size_t)p->d;
   L->shares_h = bf16 ? fef::grad_h_shares(L->rows, p->d, p->V) : fef::grad_f32_shares(L->rows, p->d, p->V);
   size_t o = 0;
   auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
-  L->off_z = take((size_t)L->rows * L->ldl * 4);
+  L->off_z = take((size_t)(bf16 ? L->rows : L->padded) * L->ldl * 4);
   L->off_partials = take((size_t)L->rows * L->nT * sizeof(float2));
   L->off_g = bf16 ? take((size_t)L->padded * L->ldl * 2) : L->off_z;
   L->off_h = take((size_t)L->padded * d * e);
@@ -700,7 +700,7 @@ fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, con
     err = bf16 ? fef::launch_head_tiled256(a) : fef::launch_head_f32(a);
     if (err != hipSuccess) return fail(FEF_ERR_HIP, "head kernel launch: %s", hipGetErrorString(err));
     fef::GradArgs g{};
-    g.rows = rows; g.padded = bf16 ? (int)align_up((size_t)rows, 64) : rows; g.V = prm->V; g.d = prm->d; g.nT = L.nT; g.ldl = L.ldl;
+    g.rows = rows; g.padded = (int)align_up((size_t)rows, 64); g.V = prm->V; g.d = prm->d; g.nT = L.nT; g.ldl = L.ldl;
     g.z = a.logits; g.partials = a.partials; g.labels = labels + r0; g.weights = weights ? weights + r0 : nullptr; g.inv_tau = a.inv_tau;
     g.h = hb; g.H = grad_w ? ws + L.off_h : nullptr; g.G = ws + L.off_g; g.out_ce = out_ce + r0;
     err = fef::launch_grad_rows(g, bf16, stream);
@@ -727,7 +727,7 @@ fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, con
     } else {
       if (grad_h) {
         fef::ProductF32Args p{};
-        p.A = (const float*)g.G; p.lda = L.ldl; p.B = (const float*)W_vocab; p.M = rows; p.N = prm->d; p.K = prm->V;
+        p.A = (const float*)g.G; p.lda = L.ldl; p.B = (const float*)W_vocab; p.b_rows = prm->V; p.M = rows; p.N = prm->d; p.K = (int)L.ldl;
         p.shares = std::min(fef::grad_f32_shares(rows, prm->d, prm->V), L.shares_h); p.stride = stride_h;
         p.C = p.shares > 1 ? part : (float*)gh;
         err = fef::launch_grad_product_f32(p, false, stream);
@@ -735,7 +735,7 @@ fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, con
       }
       if (err == hipSuccess && grad_w) {
         fef::ProductF32Args p{};
-        p.A = (const float*)g.G; p.lda = L.ldl; p.B = (const float*)g.H; p.M = prm->V; p.N = prm->d; p.K = rows; p.shares = 1;
+        p.A = (const float*)g.G; p.lda = L.ldl; p.B = (const float*)g.H; p.b_rows = g.padded; p.M = prm->V; p.N = prm->d; p.K = (int)align_up((size_t)rows, 32); p.shares = 1;
         p.C = (float*)grad_w; p.add = b > 0;
         err = fef::launch_grad_product_f32(p, true, stream);
       }

@@ -272,8 +272,8 @@ struct ProductArgs {
 struct ProductF32Args {
   const float* A;
   long lda;
-  const float* B;  // [K, N]
-  int M, N, K;
+  const float* B;       // [b_rows, N]
+  int b_rows, M, N, K;  // K a multiple of 32; rows of B past the last, and columns of k past it in A, count as zero in A
   float* C;
   int shares;
   size_t stride;
