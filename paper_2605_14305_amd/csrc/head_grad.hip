@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "head_common.hpp"
+#include "wave_ops.hpp"
 
 namespace fef {
 namespace {
@@ -18,83 +19,102 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 // ---------------------------------------------------------------------------------------------
 // G from z
 // ---------------------------------------------------------------------------------------------
-constexpr int NT = 256, kChunk = 4096;  // tokens per workgroup
+constexpr int NT = 256, kQuads = 4, kChunk = NT * 4 * kQuads;  // tokens per workgroup
 
 // Log-sum-exp of a row from its partials, in every thread; fixed order.
 __device__ __forceinline__ float row_lse(const float2* P, int n) {
   __shared__ float2 part[NT / kWave];
   const int tid = threadIdx.x;
   float mx = kLowest, sm = 0.f;
-  for (int t = tid; t < n; t += NT) {
-    const float2 p = P[t];
-    const float m = fmaxf(mx, p.x);
-    sm = sm * expf(mx - m) + p.y * expf(p.x - m);
-    mx = m;
-  }
+  for (int t0 = tid; t0 < n; t0 += 4 * NT) {  // four loads in flight
+    float2 p[4];
 #pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const float mo = __shfl_xor(mx, d), so = __shfl_xor(sm, d);
-    const float m = fmaxf(mx, mo);
-    sm = sm * expf(mx - m) + so * expf(mo - m);
+    for (int j = 0; j < 4; ++j) p[j] = t0 + j * NT < n ? P[t0 + j * NT] : make_float2(kLowest, 0.f);
+    const float m = fmaxf(fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x)), mx);
+    sm *= expf(mx - m);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sm += p[j].y * expf(p[j].x - m);
     mx = m;
   }
-  if ((tid & 63) == 0) part[tid >> 6] = make_float2(mx, sm);
+  const float top = wave_max(mx);
+  sm = wave_sum(sm * expf(mx - top));
+  if ((tid & 63) == 0) part[tid >> 6] = make_float2(top, sm);
   __syncthreads();
-  mx = part[0].x;
-#pragma unroll
-  for (int w = 1; w < NT / kWave; ++w) mx = fmaxf(mx, part[w].x);
+  mx = fmaxf(fmaxf(part[0].x, part[1].x), fmaxf(part[2].x, part[3].x));
+  static_assert(NT / kWave == 4, "");
   sm = 0.f;
 #pragma unroll
   for (int w = 0; w < NT / kWave; ++w) sm += part[w].y * expf(part[w].x - mx);
   return mx + logf(sm);
 }
 
-// A row of G (zeros behind the vocabulary, in rows that do not count and in the rows that fill up a block of 64), and the row's loss.
-// G may be z itself (float).
+template <class T>
+__device__ __forceinline__ void store_quad(T* p, const T (&o)[4]) {
+  if constexpr (sizeof(T) == 2) {
+    uint2 u;
+    __builtin_memcpy(&u, o, 8);
+    *reinterpret_cast<uint2*>(p) = u;
+  } else {
+    *reinterpret_cast<float4*>(p) = make_float4(o[0], o[1], o[2], o[3]);
+  }
+}
+
+// A row of G (zeros behind the vocabulary, in rows that do not count and in the rows that fill up a block of 64), the row's loss, and its row
+// of H.  G may be z itself (float).
+//
+// What bounds it: z read and G written, 1.55 GB at 2048 rows of V = 126464 in 257 us (6.0 TB/s; with a quad per thread and turn 327); a few rows: the way from the partials to the
+// log-sum-exp, in whose shade the logits are read.
 template <class T>
 __global__ __launch_bounds__(NT) void grad_rows_kernel(GradArgs a) {
   const int r = blockIdx.y, tid = threadIdx.x;
-  const int v0 = blockIdx.x * kChunk, v1 = min((int)a.ldl, v0 + kChunk);
+  const int v0 = blockIdx.x * kChunk + 4 * tid;  // the thread's quads: every 4 NT tokens; a.ldl is a multiple of 64
   T* G = (T*)a.G + (size_t)r * a.ldl;
   const int label = r < a.rows ? a.labels[r] : -1;
-  if (label < 0) {  // workgroup-uniform
-    for (int v = v0 + 4 * tid; v < v1; v += 4 * NT)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) G[v + c] = (T)0.f;
-    if (blockIdx.x == 0) {
-      if (r < a.rows && tid == 0) a.out_ce[r] = 0.f;
-      if (a.H)  // (of grad_W) what such a row holds is not looked at
-        for (int k = tid; k < a.d; k += NT) ((T*)a.H)[(size_t)r * a.d + k] = (T)0.f;
+  if (blockIdx.x == 0 && a.H) {  // (of grad_W) what a row that does not count holds is not looked at
+    const T* from = (const T*)a.h + (size_t)r * a.d;
+    T* to = (T*)a.H + (size_t)r * a.d;
+    if (a.d % 4 == 0) {
+      for (int k = 4 * tid; k < a.d; k += 4 * NT) {
+        T x[4] = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
+        if (label >= 0) __builtin_memcpy(x, from + k, sizeof x);
+        store_quad(to + k, x);
+      }
+    } else {
+      for (int k = tid; k < a.d; k += NT) to[k] = label >= 0 ? from[k] : (T)0.f;
     }
+  }
+  if (label < 0) {  // workgroup-uniform
+    const T zero[4] = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q)
+      if (v0 + q * 4 * NT < a.ldl) store_quad(G + v0 + q * 4 * NT, zero);
+    if (blockIdx.x == 0 && r < a.rows && tid == 0) a.out_ce[r] = 0.f;
     return;
   }
   const float* z = a.z + (size_t)r * a.ldl;
+  floatx4 x[kQuads];
+#pragma unroll
+  for (int q = 0; q < kQuads; ++q)
+    x[q] = v0 + q * 4 * NT < a.ldl ? *reinterpret_cast<const floatx4*>(z + v0 + q * 4 * NT) : floatx4{0.f, 0.f, 0.f, 0.f};
   const float lse = row_lse(a.partials + (size_t)r * a.nT, a.nT);
   const bool known = label < a.V;
-  if (tid == 0 && known && label >= v0 && label < v1) a.out_ce[r] = lse - z[label];  // its own tokens only: G may be z
-  if (tid == 0 && !known && blockIdx.x == 0) a.out_ce[r] = __builtin_nanf("");
-  __syncthreads();
-  if (blockIdx.x == 0 && a.H)
-    for (int k = tid; k < a.d; k += NT) ((T*)a.H)[(size_t)r * a.d + k] = ((const T*)a.h)[(size_t)r * a.d + k];
-  const float g = (a.weights ? a.weights[r] : 1.f) * a.inv_tau;
-  for (int v = v0 + 4 * tid; v < v1; v += 4 * NT) {
-    const float4 x = *reinterpret_cast<const float4*>(z + v);
-    const float l[4] = {x.x, x.y, x.z, x.w};
+  if (!known && blockIdx.x == 0 && tid == 0) a.out_ce[r] = __builtin_nanf("");
+  const float g = known ? (a.weights ? a.weights[r] : 1.f) * a.inv_tau : __builtin_nanf("");
+#pragma unroll
+  for (int q = 0; q < kQuads; ++q) {
+    const int v = v0 + q * 4 * NT;
+    if (v >= a.ldl) break;
     T o[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      float p = expf(l[c] - lse);
-      if (v + c == label) p -= 1.f;
-      p *= known ? g : __builtin_nanf("");
-      o[c] = (T)(v + c < a.V ? p : 0.f);
+      float p = expf(x[q][c] - lse);
+      if (known && v + c == label) {  // an unknown label may be a place of the padding
+        p -= 1.f;
+        a.out_ce[r] = lse - x[q][c];
+      }
+      o[c] = (T)(v + c < a.V ? p * g : 0.f);
     }
-    if constexpr (sizeof(T) == 2) {
-      uint2 u;
-      __builtin_memcpy(&u, o, 8);
-      *reinterpret_cast<uint2*>(G + v) = u;
-    } else {
-      *reinterpret_cast<float4*>(G + v) = make_float4(o[0], o[1], o[2], o[3]);
-    }
+    store_quad(G + v, o);
   }
 }
 
@@ -347,7 +367,14 @@ __global__ __launch_bounds__(256) void grad_sum_kernel(const float* part, int sh
   const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (i >= n) return;
   floatx4 s = *reinterpret_cast<const floatx4*>(part + i);
-  for (int j = 1; j < shares; ++j) s += *reinterpret_cast<const floatx4*>(part + (size_t)j * stride + i);
+  for (int j0 = 1; j0 < shares; j0 += 8) {  // eight loads in flight
+    floatx4 x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const floatx4*>(part + (size_t)min(j0 + j, shares - 1) * stride + i);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j0 + j < shares) s += x[j];
+  }
 #pragma unroll
   for (int c = 0; c < 4; ++c)
     if (i + c < n) out[i + c] = (OUT)s[c];
