@@ -53,7 +53,7 @@ struct Shared {
   u64 mass[kBins];       // fixed point; after step 2: the mass above the bin, a double
   u64 list[kList];
   u64 tile[kTiles];
-  u64 part[16];
+  u64 part[32];
   double power[64];      // 2^(j / 64)
   unsigned list_n, kept;
   unsigned found[4];
@@ -131,6 +131,34 @@ __device__ __forceinline__ D block_scan(D x, D* part, D& total) {
   return w ? of_lane(w - 1) + x : x;
 }
 
+// Both at once.
+template <int T>
+__device__ __forceinline__ void block_scan2(u64& c, double& w, u64* part, u64& all, double& total) {
+  constexpr int W = T / kWave;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  c = wave_scan64(c);
+  w = wave_scan64(w);
+  lds_barrier();
+  if (lane == 63) {
+    part[wave] = c;
+    part[W + wave] = __builtin_bit_cast(u64, w);
+  }
+  lds_barrier();
+  const u64 c_sums = wave_scan64(lane < W ? part[lane < W ? lane : 0] : 0);
+  const double w_sums = wave_scan64(lane < W ? __builtin_bit_cast(double, part[lane < W ? W + lane : W]) : 0.0);
+  auto of_lane = [&](u64 b, int l) __attribute__((always_inline)) {
+    return (u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(b >> 32), l) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)b, l);
+  };
+  const u64 w_bits = __builtin_bit_cast(u64, w_sums);
+  all = of_lane(c_sums, W - 1);
+  total = __builtin_bit_cast(double, of_lane(w_bits, W - 1));
+  const int before = __builtin_amdgcn_readfirstlane(wave);
+  if (before) {
+    c += of_lane(c_sums, before - 1);
+    w += __builtin_bit_cast(double, of_lane(w_bits, before - 1));
+  }
+}
+
 template <bool BF16>
 struct Row {
   const void* x;
@@ -179,26 +207,20 @@ struct Row {
   }
 };
 
-// Tokens of vectors [begin, end) of a row, four at a time: f(first id, y[4]); ids outside of the row come as -inf, and so do those of vectors
-// that are not wanted.  Wavefronts stay whole.
-template <int T, int U, bool BF16, class F, class W>
-__device__ __forceinline__ void each(const Row<BF16>& r, int begin, int end, F f, W wanted) {
+// Tokens of vectors [begin, end) of a row, four at a time: f(first id, y[4]); ids outside of the row come as -inf.  Wavefronts stay whole.
+template <int T, int U, bool BF16, class F>
+__device__ __forceinline__ void each(const Row<BF16>& r, int begin, int end, F f) {
   const int lane = threadIdx.x & 63;
   for (int j0 = begin + (int)threadIdx.x - lane; j0 < end; j0 += U * T) {
     float y[U][4];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (j0 + u * T < end) {
-        if (wanted(j0 + u * T + lane)) r.load(j0 + u * T + lane, y[u]);
-        else y[u][0] = y[u][1] = y[u][2] = y[u][3] = -INFINITY;
-      }
+      if (j0 + u * T < end) r.load(j0 + u * T + lane, y[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (j0 + u * T < end) f(4 * (j0 + u * T + lane) - r.head, y[u]);
   }
 }
-template <int T, int U, bool BF16, class F>
-__device__ __forceinline__ void each(const Row<BF16>& r, int begin, int end, F f) { each<T, U>(r, begin, end, f, [](int) { return true; }); }
 template <int T, bool BF16, class F>
 __device__ __forceinline__ void each(const Row<BF16>& r, F f) { each<T, 4>(r, 0, r.vectors(), f); }
 
@@ -228,11 +250,11 @@ struct Bins {
 
 // Weights in [0, 4) as whole numbers of 2^-f: adding 2^(52 - f) leaves them in the low bits.
 struct Fixed {
-  double scale, magic;
+  double magic, unit;
   __device__ __forceinline__ explicit Fixed(int V) {
     const int f = min(50, 61 - (32 - __clz(V)));
-    scale = ldexp(1.0, f);
     magic = ldexp(1.0, 52 - f);
+    unit = ldexp(1.0, -f);
   }
   __device__ __forceinline__ u64 of(double w) const {
     return __builtin_bit_cast(u64, w + magic) & ((1ull << 52) - 1);
@@ -454,16 +476,28 @@ __device__ __forceinline__ bool find_zone(Shared& s, const Limits& lim, const Bi
     wi[i] = 0;
   }
   if (__ballot(any != 0)) {
+    constexpr double kDown[8] = {1.0, 0x1.f03f56a88b5d8p-1, 0x1.e0fabfbc702a4p-1, 0x1.d22e6a0197c03p-1, 0x1.c3d6a24ed8222p-1, 0x1.b5efd29f24c26p-1, 0x1.a876812c0877cp-1, 0x1.9b674f8f2f3d8p-1};  // exp(-i / 32)
+    static_assert(PER <= 8, "");
+    const double first = exp64(bins.middle(b0 - PER * tid) - (double)top, s.power);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      wi[i] = (double)mi[i] * exp64(bins.middle(b0 - PER * tid - i) - (double)top, s.power);  // of 2^-f
+      wi[i] = (double)mi[i] * (first * kDown[i]);  // of 2^-f
       w += wi[i];
     }
   }
   u64 c_here = 0, c_at = 0;
   double w_here = 0, w_at = 0;
-  if (by_k(lim)) c_at = block_scan<T>((u64)c, s.part, c_here) - c;
-  if (by_p(lim)) w_at = block_scan<T>(w, (double*)s.part, w_here) - w;
+  if (by_k(lim) && by_p(lim)) {
+    c_at = c;
+    w_at = w;
+    block_scan2<T>(c_at, w_at, s.part, c_here, w_here);
+    c_at -= c;
+    w_at -= w;
+  } else if (by_k(lim)) {
+    c_at = block_scan<T>((u64)c, s.part, c_here) - c;
+  } else {
+    w_at = block_scan<T>(w, (double*)s.part, w_here) - w;
+  }
   if (FULL || BELOW) {
     all += c_here;
     total += w_here;
@@ -516,7 +550,7 @@ __device__ __forceinline__ bool find_zone(Shared& s, const Limits& lim, const Bi
 
 // Step 3 over vectors [begin, end): out, s.tile, s.list, s.list_n (which counts on where the list is full).  Returns the tokens kept (of this
 // thread).
-template <int T, bool GROUPS = false, bool BF16>
+template <int T, bool NEAR, bool GROUPS = false, bool BF16>
 __device__ __forceinline__ unsigned keep(Shared& s, const Row<BF16>& r, int begin, int end, const Limits& lim, const Bins& bins, const Fixed& fixed,
                                          const Zone& z, float top, int tile_log, const float* groups = nullptr) {
   // y from `sure` on is kept, y below `maybe` is not; in between the bins say (and a little beside the zone, whose borders are numbers of 64 bits)
@@ -525,16 +559,17 @@ __device__ __forceinline__ unsigned keep(Shared& s, const Row<BF16>& r, int begi
   const double up = z.zone ? bins.begin(z.sure + 1) : 0, down = z.zone ? bins.begin(low_bin) : 0;
   const float sure = z.zone ? (z.sure < kBins - 1 ? fmaxf((float)(up + (1e-6 + 1e-6 * fabs(up))), least) : INFINITY) : least;
   const float maybe = z.zone ? (low_bin > 0 ? (float)(down - (1e-6 + 1e-6 * fabs(down))) : kNone) : INFINITY;
-  const float wanted = fminf(sure, maybe);
+  const float least_wanted = fminf(sure, maybe);
   unsigned kept = 0;
-  each<T, 4>(r, begin, end, [&](int v, const float(&y)[4]) __attribute__((always_inline)) {
+  auto one = [&](int v, const float(&y)[4], u64& sum) __attribute__((always_inline)) {
     float o[4];
-    bool any = false, listed = false;
+    unsigned mine = 0;
+    bool listed = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const bool keep = y[i] >= sure;
       o[i] = keep ? y[i] : -INFINITY;
-      any |= keep;
+      mine |= (unsigned)keep << i;
       listed |= y[i] >= maybe && !keep;
     }
     if (listed) {
@@ -548,7 +583,7 @@ __device__ __forceinline__ unsigned keep(Shared& s, const Row<BF16>& r, int begi
         n += is[i];
         if (token && bin > z.sure && y[i] >= least) {
           o[i] = y[i];
-          any = true;
+          mine |= 1u << i;
         }
       }
       if (n) {
@@ -561,30 +596,41 @@ __device__ __forceinline__ unsigned keep(Shared& s, const Row<BF16>& r, int begi
           }
       }
     }
-    if (__ballot(any)) {
-      u64 w[4], sum = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i] = o[i] > -INFINITY ? fixed.of(exp64((double)o[i] - (double)top, s.power)) : 0;
-        kept += o[i] > -INFINITY;
-        sum += w[i];
-      }
-      const int p0 = r.position(v) - 4 * (int)(threadIdx.x & 63);  // of the wavefront
-      if (p0 >> tile_log == (p0 + 255) >> tile_log) {
-        sum = wave_scan64(sum);
-        if ((threadIdx.x & 63) == 63 && sum) atomicAdd(&s.tile[p0 >> tile_log], sum);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (w[i]) atomicAdd(&s.tile[r.position(v + i) >> tile_log], w[i]);
-      }
-    }
     if (r.out) r.template store<GROUPS>(v, o);
-  }, [&](int j) __attribute__((always_inline)) {
-    if constexpr (!GROUPS) return true;
-    const int group = (4 * j) >> kGroupLog;
-    return group >= kGroups || groups[group] >= wanted;
-  });
+    kept += __popc(mine);
+    for (; mine; mine &= mine - 1) {  // few lanes have more than one
+      const float x = mine & 1 ? y[0] : mine & 2 ? y[1] : mine & 4 ? y[2] : y[3];
+      sum += fixed.of(exp64((double)x - (double)top, s.power));
+    }
+  };
+  // NEAR: a wavefront takes 1024 neighbouring positions at a time, which lie in one tile; else, for short rows, 256, so that all have work.
+  constexpr int U = 4, kApart = NEAR ? 64 : T;
+  const int lane = threadIdx.x & 63;
+  for (int j0 = begin + (NEAR ? U : 1) * ((int)threadIdx.x - lane); j0 < end; j0 += U * T) {
+    float y[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + kApart * u + lane;
+      bool wanted = j0 + kApart * u < end;
+      if constexpr (GROUPS) wanted = wanted && ((4 * j) >> kGroupLog >= kGroups || groups[(4 * j) >> kGroupLog] >= least_wanted);
+      if (wanted) r.load(j, y[u]);
+      else y[u][0] = y[u][1] = y[u][2] = y[u][3] = -INFINITY;
+    }
+    u64 sum = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (j0 + kApart * u < end) {
+        one(4 * (j0 + kApart * u + lane) - r.head, y[u], sum);
+        if constexpr (!NEAR) {
+          if (sum) atomicAdd(&s.tile[(4 * (j0 + kApart * u + lane)) >> tile_log], sum);
+          sum = 0;
+        }
+      }
+    if (NEAR && __ballot(sum != 0)) {
+      sum = wave_scan64(sum);
+      if (lane == 63) atomicAdd(&s.tile[(4 * j0) >> tile_log], sum);
+    }
+  }
   return kept;
 }
 
@@ -593,30 +639,44 @@ template <int T, bool BF16>
 __device__ __forceinline__ void resolve(Shared& s, const Row<BF16>& r, const Limits& lim, const Bins& bins, const Fixed& fixed, const Zone& z,
                                         float top, int tile_log, unsigned n, unsigned& last, int& last_id) {
   const int tid = threadIdx.x;
-  unsigned size = 2;
-  while (size < n) size <<= 1;
-  for (unsigned i = n + tid; i < size; i += T) s.list[i] = 0;
-  lds_barrier();
-  auto exchange = [&](unsigned i, unsigned k, unsigned d) __attribute__((always_inline)) {
-    const unsigned x = 2 * i - (i & (d - 1)), y = x + d;
-    const u64 p = s.list[x], q = s.list[y];
-    if ((p < q) == ((x & k) == 0)) {  // descending
-      s.list[x] = q;
-      s.list[y] = p;
+  if (n <= T) {  // an entry's place is how many are larger (no two are equal): `parts` threads of different wavefronts count for each
+    unsigned size = 64;
+    while (size < n) size <<= 1;
+    const unsigned parts = T / size, part = tid / size, e = tid & (size - 1);
+    const unsigned each = ((n + parts - 1) / parts + 7) & ~7u;  // entries that a part looks at, in eights: zeros behind the last
+    static_assert(kList >= 2 * T, "");
+    unsigned* const place = reinterpret_cast<unsigned*>(s.cnt);
+    if (tid < (int)size) place[tid] = 0;
+    const u64 mine = e < n ? s.list[e] : 0;
+    for (unsigned j = n + tid; j < parts * each; j += T) s.list[j] = 0;
+    lds_barrier();
+    unsigned larger = 0;
+    for (unsigned j = part * each; j < (part + 1) * each; j += 8) {
+      u64 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = s.list[j + i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) larger += x[i] > mine;
     }
-  };
-  if (size <= 128) {  // one wavefront, whose LDS operations keep their order
-    if (tid < 64)
-      for (unsigned k = 2; k <= size; k <<= 1)
-        for (unsigned d = k >> 1; d; d >>= 1) {
-          if (tid < (int)size / 2) exchange(tid, k, d);
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        }
+    if (e < n && larger) atomicAdd(&place[e], larger);
+    lds_barrier();
+    if (part == 0 && e < n) s.list[place[e]] = mine;
     lds_barrier();
   } else {
+    unsigned size = T;
+    while (size < n) size <<= 1;
+    for (unsigned i = n + tid; i < size; i += T) s.list[i] = 0;
+    lds_barrier();
     for (unsigned k = 2; k <= size; k <<= 1)
       for (unsigned d = k >> 1; d; d >>= 1) {
-        for (unsigned i = tid; i < size / 2; i += T) exchange(i, k, d);
+        for (unsigned i = tid; i < size / 2; i += T) {
+          const unsigned x = 2 * i - (i & (d - 1)), y = x + d;
+          const u64 p = s.list[x], q = s.list[y];
+          if ((p < q) == ((x & k) == 0)) {  // descending
+            s.list[x] = q;
+            s.list[y] = p;
+          }
+        }
         lds_barrier();
       }
   }
@@ -677,7 +737,7 @@ __device__ __forceinline__ void resolve(Shared& s, const Row<BF16>& r, const Lim
     last = (unsigned)(e >> 32);
     last_id = (int)~(unsigned)e;
   } else {
-    last = (unsigned)(s.list[0] >> 32) + 1;
+    last = (unsigned)(s.list[0] >> 32) + 1;  // (a zone has tokens)
   }
   __syncthreads();  // waits for the stores of step 3 too, some of which these overwrite
   for (unsigned i = tid; i < kept; i += T) {
@@ -831,7 +891,6 @@ __device__ __forceinline__ void token(Shared& s, const DrawArgs& a, int row, con
   }
   if (tid == 0) {
     s.found[1] = 0x7fffffffu;
-    if (a.out_lse) a.out_lse[row] = (float)((double)top + log((double)total / fixed.scale));
     if (a.out_kept) a.out_kept[row] = (int)s.kept;
   }
   lds_barrier();
@@ -845,6 +904,8 @@ __device__ __forceinline__ void token(Shared& s, const DrawArgs& a, int row, con
     float y[4];
     const int v = p0 + 4 * tid - r.head;
     r.load((p0 >> 2) + tid, y);
+    // by a wavefront that has none of the tile's first tokens, while the others wait for theirs
+    if (p0 == tile << tile_log && tid == T - 1 && a.out_lse) a.out_lse[row] = (float)((double)top + log((double)total * fixed.unit));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       w[i] = 0;
@@ -932,16 +993,25 @@ __device__ __forceinline__ void totals(Shared& s, const Limits& lim, const Bins&
       ci[u] = by_k(lim) && b + u * T < end ? s.cnt[b + u * T] : 0;
       wi[u] = by_p(lim) && b + u * T < end ? s.mass[b + u * T] : 0;
     }
+    u64 any = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       c += ci[u];
-      if (__ballot(wi[u] != 0)) w += (double)wi[u] * exp64(bins.middle(b + u * T) - y, s.power);
+      any |= wi[u];
+    }
+    if (__ballot(any != 0)) {
+      constexpr double kUp[7] = {1.0, 0x1.0f2ebd0a80020p+23, 0x1.1f43fcc4b662cp+46, 0x1.304d6aeca254bp+69, 0x1.425982cf597cdp+92, 0x1.55779b984f3ebp+115, 0x1.69b7f55b808bap+138};  // exp(16 u)
+      constexpr int kStep = T / (16 * 32);
+      static_assert(T % (16 * 32) == 0 && (U - 1) * kStep < 7, "");
+      const double first = exp64(bins.middle(b) - y, s.power);
+#pragma unroll
+      for (int u = 0; u < U; ++u) w += (double)wi[u] * (first * kUp[u * kStep]);
     }
   }
   all = 0;
   total = 0;
-  if (by_k(lim)) block_scan<T>((u64)c, s.part, all);
-  if (by_p(lim)) block_scan<T>(w, (double*)s.part, total);
+  u64 tokens = c;
+  block_scan2<T>(tokens, w, s.part, all, total);
 }
 
 __host__ __device__ inline int tile_log_of(int V) {  // tiles of 2^this positions: at least 1024, at most kTiles of them
@@ -974,7 +1044,7 @@ __device__ __forceinline__ void left_row(const DrawArgs& a, int row, Shared& s) 
   set_least(lim, top);
   Zone z;
   find_zone<T, kBins / T, true, false>(s, lim, bins, top, kBins - 1, 0, 0.0, z);
-  const unsigned kept = keep<T>(s, r, 0, r.vectors(), lim, bins, fixed, z, top, tile_log);
+  const unsigned kept = keep<T, true>(s, r, 0, r.vectors(), lim, bins, fixed, z, top, tile_log);
   if (kept) atomicAdd(&s.kept, kept);
   lds_barrier();
   unsigned last = 0;
@@ -1022,7 +1092,7 @@ __global__ __launch_bounds__(T, HERE ? 1 : 4) void draw_rows_kernel(DrawArgs a, 
     lds_barrier();
   }
   if (here) {
-    const unsigned kept = keep<T, GROUPS>(s, r, 0, r.vectors(), lim, bins, fixed, z, top, tile_log, groups);
+    const unsigned kept = keep<T, !HERE, GROUPS>(s, r, 0, r.vectors(), lim, bins, fixed, z, top, tile_log, groups);
     if (kept) atomicAdd(&s.kept, kept);
     lds_barrier();
   }
@@ -1045,7 +1115,7 @@ __global__ __launch_bounds__(T) void draw_left_kernel(DrawArgs a, const int* lef
 }
 
 // ---- slices ------------------------------------------------------------------------------------------
-constexpr int kSliceT = 512, kMostSlices = 8;  // threads; slices of a row
+constexpr int kSliceT = 1024, kFinishT = 512, kMostSlices = 8;  // threads; slices of a row
 constexpr int kWindow = 1024;                  // bins that a slice leaves: 32 below its maximum
 
 // What a slice leaves of step 1: the topmost kWindow of its bins with tokens, which reach as far down as those of the row.
@@ -1081,11 +1151,19 @@ struct Slices {
   int n, log, tiles;  // slices per row, of 2^log positions; tiles per row
 };
 
+// What a workgroup does of `all` pieces of work: neighbours on one XCD, whose L2 holds a row from one launch to the next.  Not less than `all`: nothing.
+__device__ __forceinline__ int of_xcd(int all) {
+  const int per = (all + 7) / 8, at = (int)(blockIdx.x >> 3);
+  return at < per ? (int)(blockIdx.x & 7) * per + at : all;
+}
+
 template <bool BF16>
 __global__ __launch_bounds__(kSliceT) void draw_bins_kernel(DrawArgs a, Slices sl) {
   constexpr int T = kSliceT;
   __shared__ Shared s;
-  const int tid = threadIdx.x, row = blockIdx.x / sl.n, i = blockIdx.x % sl.n;
+  const int id = of_xcd(a.B * a.K * sl.n);
+  if (id >= a.B * a.K * sl.n) return;
+  const int tid = threadIdx.x, row = id / sl.n, i = id % sl.n;
   Row<BF16> r;
   Limits lim;
   set_up(a, row, r, lim);
@@ -1099,7 +1177,7 @@ __global__ __launch_bounds__(kSliceT) void draw_bins_kernel(DrawArgs a, Slices s
   const int begin = i << (sl.log - 2), end = min(r.vectors(), (i + 1) << (sl.log - 2));
   count<T>(s, r, begin, end, lim, bins, fixed, high);
   const float top = top_of(s, high);
-  Slice& o = sl.slice[blockIdx.x];
+  Slice& o = sl.slice[id];
   const int b0 = top >= kNone ? bins.of(top) : 0;
   if (by_k(lim) || by_p(lim)) {
     for (int j = tid; j < kWindow; j += T) {
@@ -1126,7 +1204,9 @@ template <bool BF16>
 __global__ __launch_bounds__(kSliceT) void draw_keep_kernel(DrawArgs a, Slices sl) {
   constexpr int T = kSliceT, kPer = kWindow / T;
   __shared__ Shared s;
-  const int tid = threadIdx.x, row = blockIdx.x / sl.n, at = blockIdx.x % sl.n, n = sl.n;
+  const int id = of_xcd(a.B * a.K * sl.n);
+  if (id >= a.B * a.K * sl.n) return;
+  const int tid = threadIdx.x, row = id / sl.n, at = id % sl.n, n = sl.n;
   const Slice* const slice = sl.slice + (size_t)row * n;
   RowZone& o = sl.row[row];
   Row<BF16> r;
@@ -1215,7 +1295,7 @@ __global__ __launch_bounds__(kSliceT) void draw_keep_kernel(DrawArgs a, Slices s
   if (!law) no_logits<T>(r, begin, end);
   if (!law || !here) return;
   const int tile_log = tile_log_of(a.V);
-  const unsigned kept = keep<T>(s, r, begin, end, lim, bins, Fixed(a.V), z, top, tile_log);
+  const unsigned kept = keep<T, true>(s, r, begin, end, lim, bins, Fixed(a.V), z, top, tile_log);
   if (kept) atomicAdd(&s.kept, kept);
   lds_barrier();
   const unsigned mine = s.list_n;
@@ -1225,21 +1305,45 @@ __global__ __launch_bounds__(kSliceT) void draw_keep_kernel(DrawArgs a, Slices s
     if (s.found[2] + i < kList) o.list[s.found[2] + i] = s.list[i];
   const int t0 = at << (sl.log - tile_log), t1 = min(sl.tiles, (at + 1) << (sl.log - tile_log));
   for (int t = t0 + tid; t < t1; t += T) sl.tile[(size_t)row * sl.tiles + t] = s.tile[t];
-  if (tid == 0) sl.kept[blockIdx.x] = s.kept;
+  if (tid == 0) sl.kept[id] = s.kept;
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kSliceT) void draw_finish_kernel(DrawArgs a, Slices sl) {
-  constexpr int T = kSliceT;
+__global__ __launch_bounds__(kFinishT) void draw_finish_kernel(DrawArgs a, Slices sl) {
+  constexpr int T = kFinishT;
   __shared__ Shared s;
-  const int tid = threadIdx.x, row = blockIdx.x;
+  const int tid = threadIdx.x, row = of_xcd(a.B * a.K);
+  if (row >= a.B * a.K) return;
   const RowZone& o = sl.row[row];
   Row<BF16> r;
   Limits lim;
   set_up(a, row, r, lim);
   set_powers(s);
-  if (tid == 0) s.kept = 0;
+  // everything that may be needed at once, one latency for all of it: a list behind its end, and what a row without a law or one that is
+  // left did not write, is not looked at
+  u64 list[kList / T];
+  double mass[kWindow / T];
+#pragma unroll
+  for (int i = 0; i < kList / T; ++i) list[i] = o.list[tid + i * T];
+#pragma unroll
+  for (int i = 0; i < kWindow / T; ++i) mass[i] = o.mass[tid + i * T];
+  static_assert(kTiles <= T, "");
+  const u64 tile = tid < sl.tiles ? sl.tile[(size_t)row * sl.tiles + tid] : 0;
+  const unsigned kept = tid < sl.n ? sl.kept[(size_t)row * sl.n + tid] : 0;
   const unsigned n = o.n;
+  const int high = o.high;
+  if (tid < kTiles) s.tile[tid] = tile;
+#pragma unroll
+  for (int i = 0; i < kList / T; ++i) s.list[tid + i * T] = list[i];
+#pragma unroll
+  for (int i = 0; i < kWindow / T; ++i)
+    if (high >= tid + i * T) s.mass[high - tid - i * T] = __builtin_bit_cast(u64, mass[i]);
+  if (tid == 0) {
+    s.kept = 0;
+    s.above_k = o.above_k;
+  }
+  lds_barrier();
+  if (tid < sl.n) atomicAdd(&s.kept, kept);
   if (!o.law) {
     no_token(a, row);
     return;
@@ -1252,14 +1356,6 @@ __global__ __launch_bounds__(kSliceT) void draw_finish_kernel(DrawArgs a, Slices
   const float top = o.top;
   const Bins bins{o.ref};
   lim.least = o.least;
-  for (int j = tid; j < kTiles; j += T) s.tile[j] = j < sl.tiles ? sl.tile[(size_t)row * sl.tiles + j] : 0;
-  for (unsigned j = tid; j < n; j += T) s.list[j] = o.list[j];
-  if (by_p(lim))
-    for (int j = tid; j < kWindow; j += T)
-      if (o.high >= j) s.mass[o.high - j] = __builtin_bit_cast(u64, o.mass[j]);
-  if (tid == 0) s.above_k = o.above_k;
-  lds_barrier();
-  if (tid < sl.n) atomicAdd(&s.kept, sl.kept[(size_t)row * sl.n + tid]);
   lds_barrier();
   const Fixed fixed(a.V);
   const int tile_log = tile_log_of(a.V);
@@ -1300,9 +1396,9 @@ hipError_t launch_draw(const DrawArgs& a) {
   auto run = [&](auto bf16) {
     constexpr bool B16 = decltype(bf16)::value;
     if (n) {
-      hipLaunchKernelGGL(draw_bins_kernel<B16>, dim3((unsigned)n), dim3(kSliceT), 0, a.stream, a, sl);
-      hipLaunchKernelGGL(draw_keep_kernel<B16>, dim3((unsigned)n), dim3(kSliceT), 0, a.stream, a, sl);
-      hipLaunchKernelGGL(draw_finish_kernel<B16>, dim3(rows), dim3(kSliceT), 0, a.stream, a, sl);
+      hipLaunchKernelGGL(draw_bins_kernel<B16>, dim3((unsigned)((n + 7) / 8 * 8)), dim3(kSliceT), 0, a.stream, a, sl);
+      hipLaunchKernelGGL(draw_keep_kernel<B16>, dim3((unsigned)((n + 7) / 8 * 8)), dim3(kSliceT), 0, a.stream, a, sl);
+      hipLaunchKernelGGL(draw_finish_kernel<B16>, dim3((rows + 7) / 8 * 8), dim3(kFinishT), 0, a.stream, a, sl);
     } else if (a.V < kShort) {
       hipLaunchKernelGGL((draw_rows_kernel<512, B16, true>), dim3(rows), dim3(512), 0, a.stream, a, left);
     } else {
