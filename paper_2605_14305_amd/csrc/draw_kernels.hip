@@ -35,6 +35,7 @@ typedef unsigned long long u64;
 
 constexpr int kBins = 4096, kList = 2048, kTiles = 512;
 constexpr int kManyRows = 128, kShort = 16384;
+constexpr unsigned kFew = 512;
 constexpr int kGroupLog = 6, kGroups = 2816;  // positions of a row in groups of 64, of which step 3 reads those with a token that may be kept
 constexpr float kWidth = 32.f;  // bins per unit of y
 constexpr double kReached = 1 - 0x1p-44;  // of a mass: sums that meet top_p exactly (equal logits) are not missed for their last bits
@@ -267,6 +268,7 @@ struct Limits {
   unsigned least;  // smallest key that min-p keeps
   float min_p;     // 0: none
   bool law;
+  bool few;        // top-p after a small top-k: the whole list of top-k is sorted, and no bin's mass is needed
 };
 
 struct Zone {
@@ -376,9 +378,11 @@ __device__ __forceinline__ void set_up(const DrawArgs& a, int row, Row<BF16>& r,
   }
   if (lim.p <= 0 || lim.min_p > 1.f) lim.k = 1;
   if (lim.k == 1) lim.p = 2.0;
+  lim.few = lim.p < 1 && lim.k > 0 && lim.k <= kFew;
 }
 __device__ __forceinline__ bool by_k(const Limits& l) { return l.k > 0; }
 __device__ __forceinline__ bool by_p(const Limits& l) { return l.p < 1; }
+__device__ __forceinline__ bool by_mass(const Limits& l) { return by_p(l) && !l.few; }
 
 __device__ __forceinline__ void set_powers(Shared& s) {
   if (threadIdx.x < 64) s.power[threadIdx.x] = exp2(threadIdx.x * (1.0 / 64));
@@ -424,9 +428,9 @@ __device__ __forceinline__ void count(Shared& s, const Row<BF16>& r, int begin, 
   };
   using Yes = std::true_type;
   using No = std::false_type;
-  if (by_k(lim) && by_p(lim)) run(Yes{}, Yes{});
+  if (by_k(lim) && by_mass(lim)) run(Yes{}, Yes{});
   else if (by_k(lim)) run(Yes{}, No{});
-  else if (by_p(lim)) run(No{}, Yes{});
+  else if (by_mass(lim)) run(No{}, Yes{});
   else run(No{}, No{});
   if (low) atomicAdd(&s.cnt[0], low);
 }
@@ -458,7 +462,7 @@ template <int T, int PER, bool FULL, bool BELOW>
 __device__ __forceinline__ bool find_zone(Shared& s, const Limits& lim, const Bins& bins, float top, int b0, u64 all, double total, Zone& z) {
   z = Zone{-1, kBins, -1, -1, 0, 0};
   const int tid = threadIdx.x;
-  if (!by_k(lim) && !by_p(lim)) return true;
+  if (!by_k(lim) && !by_mass(lim)) return true;
   unsigned c = 0, ci[PER];
   double w = 0, wi[PER];
   u64 mi[PER];
@@ -466,7 +470,7 @@ __device__ __forceinline__ bool find_zone(Shared& s, const Limits& lim, const Bi
   for (int i = 0; i < PER; ++i) {
     const int bin = b0 - PER * tid - i;
     ci[i] = by_k(lim) && bin >= 0 ? s.cnt[bin] : 0;
-    mi[i] = by_p(lim) && bin > 0 ? s.mass[bin] : 0;
+    mi[i] = by_mass(lim) && bin > 0 ? s.mass[bin] : 0;
     c += ci[i];
   }
   u64 any = 0;
@@ -487,7 +491,7 @@ __device__ __forceinline__ bool find_zone(Shared& s, const Limits& lim, const Bi
   }
   u64 c_here = 0, c_at = 0;
   double w_here = 0, w_at = 0;
-  if (by_k(lim) && by_p(lim)) {
+  if (by_k(lim) && by_mass(lim)) {
     c_at = c;
     w_at = w;
     block_scan2<T>(c_at, w_at, s.part, c_here, w_here);
@@ -524,7 +528,7 @@ __device__ __forceinline__ bool find_zone(Shared& s, const Limits& lim, const Bi
   bool here = ends || !by_k(lim) || lim.k >= all;
   z.bin_k = ends ? (int)s.found[0] : -1;
   z.above_k = ends ? s.value[0] : total;
-  if (by_p(lim)) {
+  if (by_mass(lim)) {
     // with the mass top-k leaves somewhere in [lowest, highest], and a little room for the sums' rounding
     const double lowest = lim.p * z.above_k * (1 - 1e-12), highest = lim.p * (ends ? s.value[1] : total) * (1 + 1e-12);
 #pragma unroll
@@ -542,7 +546,7 @@ __device__ __forceinline__ bool find_zone(Shared& s, const Limits& lim, const Bi
     if (ends && z.p_low < z.bin_k) z.p_low = z.bin_k;
     if (ends && z.p_high < z.bin_k) z.p_high = z.bin_k;
   }
-  z.sure = by_p(lim) ? z.p_high : z.bin_k;
+  z.sure = lim.few ? kBins : by_mass(lim) ? z.p_high : z.bin_k;
   z.zone = by_p(lim) || z.bin_k >= 0;
   if (tid == 0 && z.bin_k >= 0) s.above_k = s.cnt[z.bin_k];
   return here;
@@ -555,7 +559,7 @@ __device__ __forceinline__ unsigned keep(Shared& s, const Row<BF16>& r, int begi
                                          const Zone& z, float top, int tile_log, const float* groups = nullptr) {
   // y from `sure` on is kept, y below `maybe` is not; in between the bins say (and a little beside the zone, whose borders are numbers of 64 bits)
   const float least = fmaxf(kNone, lim.least ? of_key(lim.least) : kNone);
-  const int low_bin = by_p(lim) ? (z.bin_k >= 0 ? min(z.bin_k, z.p_low) : z.p_low) : z.bin_k;
+  const int low_bin = by_mass(lim) ? (z.bin_k >= 0 ? min(z.bin_k, z.p_low) : z.p_low) : z.bin_k;
   const double up = z.zone ? bins.begin(z.sure + 1) : 0, down = z.zone ? bins.begin(low_bin) : 0;
   const float sure = z.zone ? (z.sure < kBins - 1 ? fmaxf((float)(up + (1e-6 + 1e-6 * fabs(up))), least) : INFINITY) : least;
   const float maybe = z.zone ? (low_bin > 0 ? (float)(down - (1e-6 + 1e-6 * fabs(down))) : kNone) : INFINITY;
@@ -579,7 +583,7 @@ __device__ __forceinline__ unsigned keep(Shared& s, const Row<BF16>& r, int begi
       for (int i = 0; i < 4; ++i) {
         const int bin = bins.of(y[i]);
         const bool token = y[i] >= maybe && y[i] >= kNone && !(y[i] >= sure);
-        is[i] = token && (z.in_k(bin) || (by_p(lim) && z.in_p(bin)));
+        is[i] = token && (lim.few ? bin >= z.bin_k : z.in_k(bin) || (by_mass(lim) && z.in_p(bin)));
         n += is[i];
         if (token && bin > z.sure && y[i] >= least) {
           o[i] = y[i];
@@ -598,6 +602,14 @@ __device__ __forceinline__ unsigned keep(Shared& s, const Row<BF16>& r, int begi
     }
     if (r.out) r.template store<GROUPS>(v, o);
     kept += __popc(mine);
+    if (__ballot(mine == 15)) {  // much is kept: four at a time
+      u64 w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = fixed.of(exp64((double)y[i] - (double)top, s.power));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum += mine >> i & 1 ? w[i] : 0;
+      mine = 0;
+    }
     for (; mine; mine &= mine - 1) {  // few lanes have more than one
       const float x = mine & 1 ? y[0] : mine & 2 ? y[1] : mine & 4 ? y[2] : y[3];
       sum += fixed.of(exp64((double)x - (double)top, s.power));
@@ -681,19 +693,22 @@ __device__ __forceinline__ void resolve(Shared& s, const Row<BF16>& r, const Lim
       }
   }
   auto y_of = [&](unsigned i) __attribute__((always_inline)) { return of_key((unsigned)(s.list[i] >> 32)); };
-  // sums[i]: weights of the entries in front of entry i, each relative to its own bin's middle; thread t has `per` neighbours
+  // sums[i]: weights of the entries in front of entry i, each relative to its own bin's middle (few: to the maximum); thread t has `per` neighbours
   u64* const sums = reinterpret_cast<u64*>(s.cnt);
   static_assert(sizeof s.cnt >= kList * sizeof(u64), "");
   const unsigned per = (n + T - 1) / T, i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  auto weight_of = [&](unsigned i) __attribute__((always_inline)) {
+    return fixed.of(lim.few ? exp64((double)y_of(i) - (double)top, s.power) : bins.weight(y_of(i)));
+  };
   if (by_p(lim)) {
     u64 mine = 0, all;
     for (unsigned i = i0; i < i1; ++i) {
-      mine += fixed.of(bins.weight(y_of(i)));
+      mine += weight_of(i);
     }
     u64 before = block_scan<T>(mine, s.part, all) - mine;
     for (unsigned i = i0; i < i1; ++i) {
       sums[i] = before;
-      before += fixed.of(bins.weight(y_of(i)));
+      before += weight_of(i);
     }
     if (tid == 0) s.last_sum = all;
     lds_barrier();
@@ -710,11 +725,14 @@ __device__ __forceinline__ void resolve(Shared& s, const Row<BF16>& r, const Lim
   };
   double target = INFINITY;
   unsigned k_first = 0, k_end = n;  // entries of bin_k that top-k leaves end at k_end
-  if (z.bin_k >= 0) {
+  if (lim.few) {
+    k_end = min(n, lim.k);
+    target = lim.p * kReached * (double)(k_end < n ? sums[k_end] : s.last_sum);
+  } else if (z.bin_k >= 0) {
     k_first = begin_of(z.bin_k);
     k_end = min(n, k_first + (lim.k - s.above_k));
   }
-  if (by_p(lim)) {
+  if (by_mass(lim)) {
     double left = z.above_k;
     if (z.bin_k >= 0) left += (double)((k_end < n ? sums[k_end] : s.last_sum) - sums[k_first]) * exp64(bins.middle(z.bin_k) - (double)top, s.power);
     target = lim.p * kReached * left;
@@ -723,7 +741,9 @@ __device__ __forceinline__ void resolve(Shared& s, const Row<BF16>& r, const Lim
   for (unsigned i = i0; i < min(i1, k_end); ++i) {
     const float y = y_of(i);
     bool is = key_of(y) >= lim.least;
-    if (by_p(lim)) {
+    if (lim.few) {
+      is = is && (double)sums[i] < target;
+    } else if (by_p(lim)) {
       const int bin = bins.of(y);
       is = is && __builtin_bit_cast(double, s.mass[bin]) + (double)(sums[i] - sums[begin_of(bin)]) * exp64(bins.middle(bin) - (double)top, s.power) < target;
     }
@@ -991,7 +1011,7 @@ __device__ __forceinline__ void totals(Shared& s, const Limits& lim, const Bins&
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       ci[u] = by_k(lim) && b + u * T < end ? s.cnt[b + u * T] : 0;
-      wi[u] = by_p(lim) && b + u * T < end ? s.mass[b + u * T] : 0;
+      wi[u] = by_mass(lim) && b + u * T < end ? s.mass[b + u * T] : 0;
     }
     u64 any = 0;
 #pragma unroll
@@ -1026,6 +1046,7 @@ __device__ __forceinline__ void left_row(const DrawArgs& a, int row, Shared& s) 
   Row<BF16> r;
   Limits lim;
   set_up(a, row, r, lim);
+  lim.few = false;
   set_powers(s);
   const Fixed fixed(a.V);
   const int tile_log = tile_log_of(a.V);
@@ -1179,10 +1200,10 @@ __global__ __launch_bounds__(kSliceT) void draw_bins_kernel(DrawArgs a, Slices s
   const float top = top_of(s, high);
   Slice& o = sl.slice[id];
   const int b0 = top >= kNone ? bins.of(top) : 0;
-  if (by_k(lim) || by_p(lim)) {
+  if (by_k(lim) || by_mass(lim)) {
     for (int j = tid; j < kWindow; j += T) {
       const int bin = b0 - j;
-      o.bin[j] = {by_p(lim) && bin >= 0 ? s.mass[bin] : 0, by_k(lim) && bin >= 0 ? s.cnt[bin] : 0, 0};
+      o.bin[j] = {by_mass(lim) && bin >= 0 ? s.mass[bin] : 0, by_k(lim) && bin >= 0 ? s.cnt[bin] : 0, 0};
     }
     u64 all;
     double total;
@@ -1236,7 +1257,7 @@ __global__ __launch_bounds__(kSliceT) void draw_keep_kernel(DrawArgs a, Slices s
   bool here = true;
   if (law) {
     set_least(lim, top);
-    if (by_k(lim) || by_p(lim)) {
+    if (by_k(lim) || by_mass(lim)) {
       for (int i = 0; i < n; ++i) {
         all += s.list[64 + i];
         total += __builtin_bit_cast(double, s.list[128 + i]);
@@ -1288,7 +1309,7 @@ __global__ __launch_bounds__(kSliceT) void draw_keep_kernel(DrawArgs a, Slices s
       o.above_k = s.above_k;
       o.z = z;
     }
-    if (z.zone && by_p(lim))
+    if (z.zone && by_mass(lim))
 #pragma unroll
       for (int q = 0; q < kPer; ++q) o.mass[kPer * tid + q] = b0 >= kPer * tid + q ? __builtin_bit_cast(double, s.mass[b0 - kPer * tid - q]) : 0;
   }
