@@ -369,9 +369,10 @@ fef_status fef_verify_logits(const fef_params* prm, const float* logits, int64_t
  *   the tokens with w >= min_p (that is, a probability of min_p times the largest one or more)
  * and the first token always.  A limit that is NaN, top_k <= 0, top_p >= 1 and min_p <= 0 limit nothing.  The token drawn is
  * min{v kept : sum of w over the kept tokens up to v, in the order of the ids, >= u times the mass kept}, as everywhere in this library.
- * Masses are sums of whole numbers of 2^-s, in top_p relative to weights of neighbouring tokens (within exp(1/32), or as small as a
- * type of 64 bits allows), s = 61 - the bits of V: results do not depend on the order of the additions.  A token whose weight is below
- * 2^-(s+1) may be kept, but is not drawn.
+ * Masses are sums of whole numbers of 2^-s, s = min(50, 61 - the bits of V), so results do not depend on the order of the additions.  In
+ * top_p a weight is counted relative to the middle of its bin, 1/64 away at the most, of 32 bins per unit of y (after a top_k of 512 or less: relative
+ * to the largest, s = 49), and the masses of bins are added in 64-bit floating point in a fixed order; a mass that meets the limit to within
+ * 2^-44 of it reaches it.  A token whose weight is below 2^-(s+1) may be kept, but is not drawn.
  * A slot without tokens, one with a +inf or a NaN, and one whose temperature is negative or NaN has no law: nothing is kept, its token
  * is -1, its confidence 0, its log-sum-exp -inf, its truncated logits are -inf throughout.
  * The truncated logits can be a half of a round (fef_verify_logits), which then draws from the truncated laws. */

@@ -7,7 +7,8 @@
 //   1. read the row: its maximum, and how many tokens and how much mass lie in each of 4096 bins of width 1/32, which reach from 80 below the
 //      largest of a sample of the row to 48 above it.  Tokens below all bins are counted in the lowest one; they have no mass (exp(-64) of the
 //      largest weight and less).
-//   2. sums over the topmost bins (64 below the maximum, or 32): the bin where top-k ends, and the bins where top-p can end, given what top-k may leave.
+//   2. sums over the topmost bins (64 below the maximum, or 32): the bin where top-k ends, and the bins where top-p can end, given what top-k may
+//      leave.  After a top-k of at most kFew top-p needs no bins: all that top-k leaves goes to the list.
 //   3. read the row again: what lies above these bins is kept and written, what lies in them goes to a list, the rest is -inf.
 //   4. the list is sorted; rank and mass before each of its tokens give (T, I); what it keeps is written.
 //   5. the token: sums of the kept mass per tile of ids, then the ids of one tile.
@@ -16,11 +17,21 @@
 // 2^-f, which no order of the atomics changes.  In step 1 weights are relative to their bin's middle, |y - middle| <= 1/64, where a
 // polynomial of degree 5 is exact to 2^-45.
 //
-// Two ways through these steps.  draw_rows_kernel: a workgroup per row, from kManyRows rows on and for short vocabularies.  Fewer long rows:
-// slices of a row, a workgroup each, in three launches: draw_bins_kernel (step 1), draw_keep_kernel (steps 2 and 3: every workgroup adds up its
-// row's bins) and draw_finish_kernel (a workgroup per row: steps 4 and 5).  What this does not serve (a list longer than kList: equal logits;
-// limits that end below step 2's bins; a maximum far above the sample) is left to left_row, which narrows down the last key by readings of
-// the row, 12 bits each.
+// Two ways through these steps.  draw_rows_kernel: a workgroup per row.  Slices of a row, a workgroup each, in three launches:
+// draw_bins_kernel (step 1), draw_keep_kernel (steps 2 and 3: every workgroup adds up its row's bins) and draw_finish_kernel (a workgroup per
+// row: steps 4 and 5).  What this does not serve (a list longer than kList: equal logits; limits that end below step 2's bins; a maximum far
+// above the sample) is left to left_row, which narrows down the last key by readings of the row, 12 bits each.
+// Which way, with k = 100 and p = 0.95 / p = 0.95 alone, a workgroup per row against slices:
+//   8 rows of V = 12000 23.0 / 20.6 against 27.9 / 26.4 us, 16384 24.9 / 27.2 against 28.0 / 29.5, 24000 29.0 / 33.5 against 28.1 / 31.1: one launch
+//   below kShort tokens;
+//   64 rows of V = 126464 78 / 133 against 42 / 58 us, 128 rows 87 / 145 against 58 / 80 (V = 32000: 36 / 45 against 34 / 39), with no more slices
+//   than the 256 CUs take at once (64 rows in 8 slices each: 57 / 73).  From kManyRows on a slice would be a row.
+//
+// What bounds it.  Many rows: 512 rows of V = 151936 with k = 200, p = 0.95 163 us, 70 of them step 1 (4.4 TB/s; without limits 57: the rest are the
+// LDS atomics), 50 step 3 (the stores, 6.2 TB/s; of its reading, groups of tokens that nothing is kept of are left out), the others the steps
+// between, in which both workgroups of a CU compute; without limits 218 us, the exponentials of all tokens.  Few rows: the way through three
+// launches, 30 us for 8 rows of V = 126464 with p = 0.95 (9.6 + 11.8 + 8.4), 42 us for 35 rows of V = 100003 with k = 1000, p = 0.98; one row of V = 5000:
+// 16 us, a third each for steps 1 to 3, the list, the token.
 #include <math.h>
 
 #include <type_traits>
@@ -34,8 +45,8 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int kBins = 4096, kList = 2048, kTiles = 512;
-constexpr int kManyRows = 128, kShort = 16384;
-constexpr unsigned kFew = 512;
+constexpr int kManyRows = 129, kShort = 24576;
+constexpr unsigned kFew = 512;  // no masses in step 1: 512 rows of V = 151936 with k = 200, p = 0.95 186 -> 163 us; lists up to 512 need no sorting
 constexpr int kGroupLog = 6, kGroups = 2816;  // positions of a row in groups of 64, of which step 3 reads those with a token that may be kept
 constexpr float kWidth = 32.f;  // bins per unit of y
 constexpr double kReached = 1 - 0x1p-44;  // of a mass: sums that meet top_p exactly (equal logits) are not missed for their last bits
@@ -193,7 +204,7 @@ struct Row {
       for (int i = 0; i < 4; ++i) y[i] = v + i >= 0 && v + i < V ? at(v + i) : -INFINITY;
     }
   }
-  // STREAM: many rows, whose outputs only push the logits out of the caches (512 rows of V = 151936 245 -> 228 us)
+  // STREAM: many rows, whose outputs only push the logits out of the caches (512 rows of V = 151936 245 -> 228 us when this came in)
   template <bool STREAM>
   __device__ __forceinline__ void store(int v, const float (&y)[4]) const {
     if (out_wide && v >= 0 && v + 4 <= V) {
@@ -651,7 +662,7 @@ template <int T, bool BF16>
 __device__ __forceinline__ void resolve(Shared& s, const Row<BF16>& r, const Limits& lim, const Bins& bins, const Fixed& fixed, const Zone& z,
                                         float top, int tile_log, unsigned n, unsigned& last, int& last_id) {
   const int tid = threadIdx.x;
-  if (n <= T) {  // an entry's place is how many are larger (no two are equal): `parts` threads of different wavefronts count for each
+  if (n <= T) {  // an entry's place is how many are larger (no two are equal): `parts` threads of different wavefronts count for each (some 60 entries: 2.3 us less than sorting them)
     unsigned size = 64;
     while (size < n) size <<= 1;
     const unsigned parts = T / size, part = tid / size, e = tid & (size - 1);
@@ -697,8 +708,9 @@ __device__ __forceinline__ void resolve(Shared& s, const Row<BF16>& r, const Lim
   u64* const sums = reinterpret_cast<u64*>(s.cnt);
   static_assert(sizeof s.cnt >= kList * sizeof(u64), "");
   const unsigned per = (n + T - 1) / T, i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  const Fixed fine(kList);  // fewer weights than a row has, in smaller units
   auto weight_of = [&](unsigned i) __attribute__((always_inline)) {
-    return fixed.of(lim.few ? exp64((double)y_of(i) - (double)top, s.power) : bins.weight(y_of(i)));
+    return lim.few ? fine.of(exp64((double)y_of(i) - (double)top, s.power)) : fixed.of(bins.weight(y_of(i)));
   };
   if (by_p(lim)) {
     u64 mine = 0, all;
@@ -1136,7 +1148,8 @@ __global__ __launch_bounds__(T) void draw_left_kernel(DrawArgs a, const int* lef
 }
 
 // ---- slices ------------------------------------------------------------------------------------------
-constexpr int kSliceT = 1024, kFinishT = 512, kMostSlices = 8;  // threads; slices of a row
+constexpr int kSliceT = 1024, kFinishT = 512;   // threads (slices of 35 rows of V = 100003 with 512: 48.2 us, with 1024: 45.5)
+constexpr int kMostSlices = 8, kCus = 256;     // of a row (16 for 8 rows: bins 10.7 -> 8.5 us, adding them up and the list 12.0 -> 13.0); of the card
 constexpr int kWindow = 1024;                  // bins that a slice leaves: 32 below its maximum
 
 // What a slice leaves of step 1: the topmost kWindow of its bins with tokens, which reach as far down as those of the row.
@@ -1172,7 +1185,8 @@ struct Slices {
   int n, log, tiles;  // slices per row, of 2^log positions; tiles per row
 };
 
-// What a workgroup does of `all` pieces of work: neighbours on one XCD, whose L2 holds a row from one launch to the next.  Not less than `all`: nothing.
+// What a workgroup does of `all` pieces of work: neighbours on one XCD, whose L2 holds a row and its bins from one launch to the next (35 rows of
+// V = 100003 45.5 -> 39.5 us).  Not less than `all`: nothing.
 __device__ __forceinline__ int of_xcd(int all) {
   const int per = (all + 7) / 8, at = (int)(blockIdx.x >> 3);
   return at < per ? (int)(blockIdx.x & 7) * per + at : all;
@@ -1390,7 +1404,8 @@ __global__ __launch_bounds__(kFinishT) void draw_finish_kernel(DrawArgs a, Slice
 int slices_of(int rows, int V, int* log) {
   *log = 12 > tile_log_of(V) ? 12 : tile_log_of(V);
   if (rows >= kManyRows || V < kShort) return 0;
-  while (((long)V + 3 + (1L << *log) - 1) >> *log > kMostSlices) ++*log;
+  const int most = kCus / rows < kMostSlices ? kCus / rows : kMostSlices;
+  while (((long)V + 3 + (1L << *log) - 1) >> *log > most) ++*log;
   return (int)(((long)V + 3 + (1L << *log) - 1) >> *log);
 }
 int tiles_of(int V) { return (int)(((long)V + 3 + (1L << tile_log_of(V)) - 1) >> tile_log_of(V)); }

@@ -148,10 +148,11 @@ __device__ __forceinline__ bf16x8 both(bf16x4 a, bf16x4 b) { return __builtin_sh
 // What bounds it: LDS and the matrix units alike.  A half of 256 x 256 x 32 takes 1024 cycles of multiplies, and with eight wavefronts of
 // 128 x 64 96 KB of fragments and 32 KB on their way in, 1024 cycles of LDS.  Four wavefronts of 128 x 128 read 64 KB, but with one wavefront per
 // SIMD every other instruction holds the multiplies: grad_h of 2048 rows of d = 4096, V = 126464 1655 -> 1931 us, grad_w 1963 -> 2092.
-//   grad_h (WN = 4): few long tiles.  1655 us = 1.28 PFLOP/s (fragments read where they are multiplied, one step ahead: 1816).
+//   grad_h (WN = 4): few long tiles.  1655 to 1760 us = 1.21 to 1.28 PFLOP/s, with the card's clock (fragments read where they are multiplied, one
+//     step ahead: 1816).
 //   grad_w (WN = 2, 128 x 256): K is the number of rows, so a tile is short, and filling the rings and writing 64 KB weigh as much as the
-//     multiplies.  Two workgroups per CU, in 72 KB each, work under each other's ends: 1903 us = 1.11 PFLOP/s, against 1963 with one of
-//     256 x 256; 48 rows 290 -> 273 (3.8 TB/s written), 333 rows of d = 2048, V = 50257 128 -> 112.
+//     multiplies.  Two workgroups per CU, in 72 KB each, work under each other's ends: 1870 to 1950 us = 1.09 to 1.13 PFLOP/s, against 1963 with
+//     one of 256 x 256; 48 rows 290 -> 273, 333 rows of d = 2048, V = 50257 128 -> 112 (with stores past the caches 263 and 102).
 template <int NR, int WN, bool AT, class OUT>
 __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel(ProductArgs a) {
   constexpr int BM = 16 * NR * WM, kWaves = WM * WN, kThreads = kWave * kWaves, kColumns = BN / WN / 16;
@@ -407,7 +408,8 @@ hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t 
   return hipGetLastError();
 }
 
-// grad_H: rows of H to a tile, and into how many shares k (the tokens) is cut so that the CUs have work.
+// grad_H: rows of H to a tile (rows that do not exist are multiplied all the same: 48 rows of V = 126464 in tiles of 64 176 us, W read at 5.9 TB/s),
+// and into how many shares k (the tokens) is cut so that the CUs have work.
 static int grad_h_rows(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 int grad_h_shares(int rows, int d, int V) {
   const int bm = grad_h_rows(rows);
