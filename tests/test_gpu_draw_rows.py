@@ -17,6 +17,15 @@ def test_many_rows(B, K, V, dtype, which):
     _check(x, _u(B, K, which), tau=0.7, **_limits(LIMITS[which], B))
 
 
+@pytest.mark.parametrize("V", [700, 9000, 30000])
+def test_top_p_after_top_k(V):
+    """Around the largest top-k whose list alone decides top-p; where fewer tokens exist than it asks for; with min-p."""
+    ks = [2, 3, 64, 255, 511, 512, 513, 700, 1500]
+    x = _x(len(ks), 2, V, V)
+    x[:, 1, 400:] = -INF
+    _check(x, _u(len(ks), 2, V), top_k=ks, top_p=[(0.9, 0.5, 0.999)[b % 3] for b in range(len(ks))], min_p=[(0.0, 1e-4)[b % 2] for b in range(len(ks))])
+
+
 def test_many_rows_longer_than_the_groups():
     """2816 groups of 64 tokens: what lies behind token 180224 is read again whatever it holds."""
     B, V = 128, 200003
