@@ -832,13 +832,33 @@ fef_status check_draw(const fef_draw_params* p, size_t* total) {
   if (p->B < 1 || p->V < 1) return fail(FEF_ERR_INVALID_ARG, "B and V must be >= 1 (got %d, %d)", p->B, p->V);
   if (p->V > kMaxGivenV) return fail(FEF_ERR_INVALID_ARG, "V = %d exceeds 2^29", p->V);
   if (p->K < 1 || p->K > FEF_MAX_K) return fail(FEF_ERR_INVALID_ARG, "K = %d out of range [1, %d]", p->K, FEF_MAX_K);
-  // (a workgroup of 1024 threads per row, and less than 2^32 threads)
+  // (a workgroup of 512 threads per row: 2^30 threads)
   if ((long)p->B * p->K > (1L << 21)) return fail(FEF_ERR_INVALID_ARG, "B*K = %ld exceeds 2^21 rows per call", (long)p->B * p->K);
   if (p->dtype != FEF_BF16 && p->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
   if (!scales_logits(p->temperature)) return fail(FEF_ERR_INVALID_ARG, "temperature must be a positive finite number with a finite reciprocal");
   for (const int64_t s : {p->seq_stride, p->slot_stride, p->out_seq_stride, p->out_slot_stride})
     if (s < 0 || s > (1L << 40)) return fail(FEF_ERR_INVALID_ARG, "strides must lie in [0, 2^40]");
   *total = align_up(fef::draw_workspace(p->B * p->K, p->V), 256);
+  return FEF_OK;
+}
+}  // namespace
+
+namespace {
+// Whether a row of `out` meets one of the logits, each of which is read several times.  Row by row only where one lies within the other's reach.
+fef_status check_draw_apart(const fef_draw_params* p, uintptr_t logits, uintptr_t out) {
+  const size_t e = p->dtype == FEF_BF16 ? 2 : 4, V = (size_t)p->V, rows = (size_t)p->B * p->K;
+  auto in = [&](size_t b, size_t m) { return logits + (b * p->seq_stride + m * p->slot_stride) * e; };
+  auto to = [&](size_t b, size_t m) { return out + (b * p->out_seq_stride + m * p->out_slot_stride) * 4; };
+  if (out >= in(p->B - 1, p->K - 1) + V * e || logits >= to(p->B - 1, p->K - 1) + V * 4) return FEF_OK;
+  std::unique_ptr<uintptr_t[]> at(new (std::nothrow) uintptr_t[rows]);
+  if (!at) return fail(FEF_ERR_UNSUPPORTED, "no host memory for the check of %zu rows", rows);
+  for (size_t r = 0; r < rows; ++r) at[r] = in(r / p->K, r % p->K);
+  std::sort(at.get(), at.get() + rows);  // all of one length: the last that begins in front of a row's end reaches furthest
+  for (size_t r = 0; r < rows; ++r) {
+    const uintptr_t begin = to(r / p->K, r % p->K), end = begin + V * 4;
+    const uintptr_t* const next = std::lower_bound(at.get(), at.get() + rows, end);
+    if (next != at.get() && next[-1] + V * e > begin) return fail(FEF_ERR_INVALID_ARG, "out must not overlap the logits: a row is read several times");
+  }
   return FEF_OK;
 }
 }  // namespace
@@ -855,8 +875,11 @@ fef_status fef_draw_logits(const fef_draw_params* p, const void* logits, float* 
   if (!logits) return fail(FEF_ERR_INVALID_ARG, "logits must not be NULL");
   if ((uintptr_t)logits & (p->dtype == FEF_BF16 ? 1 : 3) || (uintptr_t)out & 3)
     return fail(FEF_ERR_INVALID_ARG, "logits and out must be aligned to their elements");
-  if ((const void*)out == logits) return fail(FEF_ERR_INVALID_ARG, "out must not be the logits: a row is read several times");
   if (out && !rows_apart(p->B, p->K, p->V, p->out_seq_stride, p->out_slot_stride)) return fail(FEF_ERR_INVALID_ARG, "rows of the output overlap");
+  if (out) {
+    const fef_status apart = check_draw_apart(p, (uintptr_t)logits, (uintptr_t)out);
+    if (apart != FEF_OK) return apart;
+  }
   const uintptr_t lists = (uintptr_t)p->temperatures | (uintptr_t)p->top_k | (uintptr_t)p->top_p | (uintptr_t)p->min_p | (uintptr_t)p->uniforms |
                           (uintptr_t)p->out_lse | (uintptr_t)p->out_kept | (uintptr_t)p->out_tokens | (uintptr_t)p->out_conf;
   if (lists & 3) return fail(FEF_ERR_INVALID_ARG, "limits, uniforms and outputs must be 4-byte aligned");

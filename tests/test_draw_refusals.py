@@ -34,6 +34,21 @@ def test_refused_pointers(logits, out, kw):
     assert fb.lib().fef_draw_logits(ctypes.byref(_params(**kw)), logits, out) == fb.FEF_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("logits,out,kw", [(0x1000, 0x1000 + 4 * 599, {}), (0x1000 + 4 * 599, 0x1000, {}), (0x1000, 0x1000 + 4 * 299, dict(dtype=fb.FEF_BF16)),
+                                           (0x1000, 0x1000 + 4 * 100, dict(seq_stride=600, slot_stride=200, out_seq_stride=600, out_slot_stride=199)),
+                                           (0x1000, 0x1000 + 4 * 100, dict(seq_stride=0, slot_stride=0, out_seq_stride=0, out_slot_stride=0, B=1, K=1, V=101))])
+def test_an_output_that_meets_the_logits(logits, out, kw):
+    assert fb.lib().fef_draw_logits(ctypes.byref(_params(**kw)), logits, out) == fb.FEF_ERR_INVALID_ARG
+    assert "overlap" in fb.fef_last_error()
+
+
+@pytest.mark.parametrize("logits,out,kw", [(0x1000, 0x1000 + 4 * 600, {}), (0x1000 + 4 * 600, 0x1000, {}),
+                                           (0x1000, 0x1000 + 4 * 100, dict(seq_stride=600, slot_stride=200, out_seq_stride=600, out_slot_stride=200))])
+def test_an_output_beside_the_logits_gets_past_this_check(logits, out, kw):
+    """What is refused is the workspace, which is looked at later."""
+    assert fb.lib().fef_draw_logits(ctypes.byref(_params(workspace=None, **kw)), logits, out) == fb.FEF_ERR_WORKSPACE
+
+
 def test_workspace():
     need = fb.lib().fef_draw_workspace_bytes(ctypes.byref(_params()))
     assert need > 0 and need % 256 == 0
