@@ -121,7 +121,7 @@ __global__ __launch_bounds__(NT) void grad_rows_kernel(GradArgs a) {
 // ---------------------------------------------------------------------------------------------
 // C = A B, bf16 operands
 // ---------------------------------------------------------------------------------------------
-constexpr int BN = 256, BK = 64, HK = 32, WM = 2;
+constexpr int BN = 256, BK = 64, HK = 32, WM = 2, kStrip = 8;
 
 // Rows of `cols` columns in LDS, a row per k, 32 bytes (16 columns) at chunk c ^ turn_of(k): the 32 lanes of half a transposed read, which take
 // 32 bytes of rows 8 g + {0, 1, 2, 3} of two lane groups g, fall on different banks.
@@ -181,7 +181,13 @@ __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel
   const long id = (long)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if ((long)(blockIdx.x >> 3) >= per || id >= tiles) return;
   const int share = (int)(id / ((long)mt * nt)), at = (int)(id % ((long)mt * nt));
-  const int m0 = (a.n_first ? at / nt : at % mt) * BM, n0 = (a.n_first ? at % nt : at / mt) * BN;
+  int tm = at % mt, tn = at / mt;
+  if (a.n_first) {
+    const int strip = at / (mt * kStrip), first = strip * kStrip, wide = min(kStrip, nt - first), in = at - mt * first;
+    tm = in / wide;
+    tn = first + in % wide;
+  }
+  const int m0 = tm * BM, n0 = tn * BN;
   const int nk_all = a.K / BK;
   const int k0 = (int)((long)share * nk_all / a.shares), nk = (int)((long)(share + 1) * nk_all / a.shares) - k0, nh = 2 * nk;
 
