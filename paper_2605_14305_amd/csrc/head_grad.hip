@@ -121,7 +121,7 @@ __global__ __launch_bounds__(NT) void grad_rows_kernel(GradArgs a) {
 // ---------------------------------------------------------------------------------------------
 // C = A B, bf16 operands
 // ---------------------------------------------------------------------------------------------
-constexpr int BN = 256, BK = 64, HK = 32, WM = 2, kStrip = 8;
+constexpr int BN = 256, BK = 64, HK = 32, WM = 2, kStrip = 4;
 
 // Rows of `cols` columns in LDS, a row per k, 32 bytes (16 columns) at chunk c ^ turn_of(k): the 32 lanes of half a transposed read, which take
 // 32 bytes of rows 8 g + {0, 1, 2, 3} of two lane groups g, fall on different banks.
@@ -151,8 +151,10 @@ __device__ __forceinline__ bf16x8 both(bf16x4 a, bf16x4 b) { return __builtin_sh
 //   grad_h (WN = 4): few long tiles.  1655 to 1760 us = 1.21 to 1.28 PFLOP/s, with the card's clock (fragments read where they are multiplied, one
 //     step ahead: 1816).
 //   grad_w (WN = 2, 128 x 256): K is the number of rows, so a tile is short, and filling the rings and writing 64 KB weigh as much as the
-//     multiplies.  Two workgroups per CU, in 72 KB each, work under each other's ends: 1870 to 1950 us = 1.09 to 1.13 PFLOP/s, against 1963 with
-//     one of 256 x 256; 48 rows 290 -> 273, 333 rows of d = 2048, V = 50257 128 -> 112 (with stores past the caches 263 and 102).
+//     multiplies.  Two workgroups per CU, in 72 KB each, work under each other's ends: 1903 us, against 1963 with
+//     one of 256 x 256; 48 rows 290 -> 273, 333 rows of d = 2048, V = 50257 128 -> 112 (with stores past the caches 263 and 102).  An XCD walks
+//     down a strip of kStrip tiles, whose columns of H (4 MB at 2048 rows) stay in its L2: 1740 us = 1.22 PFLOP/s, 4.3 GB read (strips of 8 tiles
+//     1785 us, 6.2 GB; rows of all 16 1898 us, 12.0 GB).
 template <int NR, int WN, bool AT, class OUT>
 __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel(ProductArgs a) {
   constexpr int BM = 16 * NR * WM, kWaves = WM * WN, kThreads = kWave * kWaves, kColumns = BN / WN / 16;
