@@ -610,12 +610,11 @@ fef_status fef_mx4_logits(const fef_params* prm, const void* h, const uint8_t* c
 }
 
 namespace {
-constexpr int kGradRows = 8192;  // rows of a block: its logits and G lie in the workspace (8.3 GB and half of that at V = 126464)
 
 struct GradLayout {
   int rows, padded, nT, shares_h, blocks;
   long ldl;
-  size_t off_z, off_partials, off_g, off_h, off_part, off_acc, total;
+  size_t off_z, off_partials, off_g, off_h, off_rest, off_part, off_acc, total;
 };
 
 fef_status grad_layout(const fef_params* p, int32_t R, GradLayout* L) {
@@ -633,8 +632,8 @@ fef_status grad_layout(const fef_params* p, int32_t R, GradLayout* L) {
   if (p->gemm_variant != FEF_GEMM_AUTO && p->gemm_variant != (bf16 ? FEF_GEMM_TILED256 : FEF_GEMM_F32))
     return fail(FEF_ERR_UNSUPPORTED, "gradients run through the TILED256 (bf16) or the F32 head kernel");
   if (p->ev_head_begin || p->ev_head_end) return fail(FEF_ERR_INVALID_ARG, "ev_head_begin and ev_head_end must be NULL in this call");
-  L->rows = R < kGradRows ? R : kGradRows;
-  L->blocks = (R + kGradRows - 1) / kGradRows;
+  L->rows = R < fef::kGradRows ? R : fef::kGradRows;
+  L->blocks = (R + fef::kGradRows - 1) / fef::kGradRows;
   L->padded = (int)align_up((size_t)L->rows, 64);
   L->ldl = (long)align_up((size_t)p->V, 64);
   L->nT = bf16 ? (p->V + fef::kTiled256Tn - 1) / fef::kTiled256Tn : (p->V + fef::kTiledTn - 1) / fef::kTiledTn;
@@ -646,6 +645,7 @@ fef_status grad_layout(const fef_params* p, int32_t R, GradLayout* L) {
   L->off_partials = take((size_t)L->rows * L->nT * sizeof(float2));
   L->off_g = bf16 ? take((size_t)L->padded * L->ldl * 2) : L->off_z;
   L->off_h = take((size_t)L->padded * d * e);
+  L->off_rest = take((size_t)L->rows * 4);
   // (a last block of fewer rows may take more shares of as many rows less)
   L->off_part = take(align_up((size_t)L->rows * d, 4) * 4 * (size_t)L->shares_h);
   L->off_acc = take(bf16 && L->blocks > 1 ? (size_t)p->V * d * 4 : 0);
@@ -687,8 +687,8 @@ fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, con
   float* const acc = (float*)(ws + L.off_acc);
   hipError_t err = hipSuccess;
   for (int b = 0; b < L.blocks; ++b) {
-    const size_t r0 = (size_t)b * kGradRows;
-    const int rows = (int)std::min((size_t)kGradRows, (size_t)R - r0);
+    const size_t r0 = (size_t)b * fef::kGradRows;
+    const int rows = (int)std::min((size_t)fef::kGradRows, (size_t)R - r0);
     const char* hb = (const char*)h + r0 * d * e;
     fef::HeadArgs a{};
     a.h_draft = a.h_target = hb; a.W = W_vocab;
@@ -703,6 +703,7 @@ fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, con
     g.rows = rows; g.padded = (int)align_up((size_t)rows, 64); g.V = prm->V; g.d = prm->d; g.nT = L.nT; g.ldl = L.ldl;
     g.z = a.logits; g.partials = a.partials; g.labels = labels + r0; g.weights = weights ? weights + r0 : nullptr; g.inv_tau = a.inv_tau;
     g.h = hb; g.H = grad_w ? ws + L.off_h : nullptr; g.G = ws + L.off_g; g.out_ce = out_ce + r0;
+    g.rest = bf16 ? (float*)(ws + L.off_rest) : nullptr;
     err = fef::launch_grad_rows(g, bf16, stream);
     if (err != hipSuccess) return fail(FEF_ERR_HIP, "gradient kernel launch: %s", hipGetErrorString(err));
     const size_t n_h = (size_t)rows * d, stride_h = align_up(n_h, 4), n_w = V * d;
@@ -710,19 +711,21 @@ fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, con
     if (bf16) {
       if (grad_h) {
         fef::ProductArgs p{};
+        p.rows = rows; p.labels = g.labels; p.rest = g.rest;
         p.A = (const __bf16*)g.G; p.lda = L.ldl; p.B = (const __bf16*)W_vocab; p.ldb = prm->d; p.b_rows = prm->V;
         p.M = rows; p.N = prm->d; p.K = (int)L.ldl; p.shares = std::min(fef::grad_h_shares(rows, prm->d, prm->V), L.shares_h); p.stride = stride_h;
         p.C = p.shares > 1 ? (void*)part : (void*)gh;
         err = fef::launch_grad_h(p, stream);
-        if (err == hipSuccess && p.shares > 1) err = fef::launch_grad_sum(part, p.shares, stride_h, n_h, gh, true, stream);
+        if (err == hipSuccess && p.shares > 1) err = fef::launch_grad_sum(part, p.shares, stride_h, n_h, gh, true, &p, stream);
       }
       if (err == hipSuccess && grad_w) {
         fef::ProductArgs p{};
+        p.rows = rows; p.labels = g.labels; p.rest = g.rest;
         p.A = (const __bf16*)g.G; p.lda = L.ldl; p.B = (const __bf16*)g.H; p.ldb = prm->d; p.b_rows = g.padded;
         p.M = prm->V; p.N = prm->d; p.K = g.padded; p.shares = 1; p.n_first = 1;
         p.C = L.blocks > 1 ? (void*)acc : grad_w; p.add = b > 0;
         err = fef::launch_grad_w(p, L.blocks > 1, stream);
-        if (err == hipSuccess && L.blocks > 1 && b + 1 == L.blocks) err = fef::launch_grad_sum(acc, 1, 0, n_w, grad_w, true, stream);
+        if (err == hipSuccess && L.blocks > 1 && b + 1 == L.blocks) err = fef::launch_grad_sum(acc, 1, 0, n_w, grad_w, true, nullptr, stream);
       }
     } else {
       if (grad_h) {
@@ -731,7 +734,7 @@ fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, con
         p.shares = std::min(fef::grad_f32_shares(rows, prm->d, prm->V), L.shares_h); p.stride = stride_h;
         p.C = p.shares > 1 ? part : (float*)gh;
         err = fef::launch_grad_product_f32(p, false, stream);
-        if (err == hipSuccess && p.shares > 1) err = fef::launch_grad_sum(part, p.shares, stride_h, n_h, gh, false, stream);
+        if (err == hipSuccess && p.shares > 1) err = fef::launch_grad_sum(part, p.shares, stride_h, n_h, gh, false, nullptr, stream);
       }
       if (err == hipSuccess && grad_w) {
         fef::ProductF32Args p{};

@@ -243,6 +243,7 @@ size_t draw_workspace(int rows, int V);
 hipError_t launch_draw(const DrawArgs& a);
 
 // Gradients of the head's cross-entropy.  G from z: rows [0, rows) of a block of rows, filled up with zero rows to `padded`.
+constexpr int kGradRows = 8192;  // rows of a block: its logits and G lie in the workspace (8.3 GB and half of that at V = 126464)
 struct GradArgs {
   int rows, padded, V, d, nT;
   long ldl;                // of z and G, a multiple of 64
@@ -255,6 +256,7 @@ struct GradArgs {
   void* H;                 // [padded, d] h with zeros in rows that do not count; NULL: not wanted
   void* G;                 // [padded, ldl], the type of h; may be z
   float* out_ce;           // [rows]
+  float* rest;  // [rows] what rounding takes from G at the label; NULL: G is float
 };
 // C[m, n] = sum_k A[m, k] B[k, n], bf16; shares > 1, or partial: float sums [shares][stride], else C is bf16
 struct ProductArgs {
@@ -268,6 +270,9 @@ struct ProductArgs {
   size_t stride;
   int add;      // partial: onto what is there
   int n_first;  // neighbouring workgroups take neighbouring columns (else rows)
+  int rows;           // of the loss, and their labels
+  const int* labels;
+  const float* rest;  // [rows] what rounding took from G at the label
 };
 struct ProductF32Args {
   const float* A;
@@ -283,7 +288,7 @@ hipError_t launch_grad_rows(const GradArgs& a, bool bf16, hipStream_t stream);
 int grad_h_shares(int rows, int d, int V);
 hipError_t launch_grad_h(const ProductArgs& a, hipStream_t stream);
 hipError_t launch_grad_w(const ProductArgs& a, bool partial, hipStream_t stream);
-hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t n, void* out, bool bf16, hipStream_t stream);
+hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t n, void* out, bool bf16, const ProductArgs* of, hipStream_t stream);
 int grad_f32_shares(int M, int N, int K);
 hipError_t launch_grad_product_f32(const ProductF32Args& a, bool at, hipStream_t stream);
 

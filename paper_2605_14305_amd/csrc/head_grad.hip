@@ -88,7 +88,10 @@ __global__ __launch_bounds__(NT) void grad_rows_kernel(GradArgs a) {
 #pragma unroll
     for (int q = 0; q < kQuads; ++q)
       if (v0 + q * 4 * NT < a.ldl) store_quad(G + v0 + q * 4 * NT, zero);
-    if (blockIdx.x == 0 && r < a.rows && tid == 0) a.out_ce[r] = 0.f;
+    if (blockIdx.x == 0 && r < a.rows && tid == 0) {
+      a.out_ce[r] = 0.f;
+      if (a.rest) a.rest[r] = 0.f;
+    }
     return;
   }
   const float* z = a.z + (size_t)r * a.ldl;
@@ -98,7 +101,10 @@ __global__ __launch_bounds__(NT) void grad_rows_kernel(GradArgs a) {
     x[q] = v0 + q * 4 * NT < a.ldl ? *reinterpret_cast<const floatx4*>(z + v0 + q * 4 * NT) : floatx4{0.f, 0.f, 0.f, 0.f};
   const float lse = row_lse(a.partials + (size_t)r * a.nT, a.nT);
   const bool known = label < a.V;
-  if (!known && blockIdx.x == 0 && tid == 0) a.out_ce[r] = __builtin_nanf("");
+  if (!known && blockIdx.x == 0 && tid == 0) {
+    a.out_ce[r] = __builtin_nanf("");
+    if (a.rest) a.rest[r] = 0.f;
+  }
   const float g = known ? (a.weights ? a.weights[r] : 1.f) * a.inv_tau : __builtin_nanf("");
 #pragma unroll
   for (int q = 0; q < kQuads; ++q) {
@@ -111,6 +117,8 @@ __global__ __launch_bounds__(NT) void grad_rows_kernel(GradArgs a) {
       if (known && v + c == label) {  // an unknown label may be a place of the padding
         p -= 1.f;
         a.out_ce[r] = lse - x[q][c];
+        const float rest = p * g - (float)(T)(p * g);
+        if (a.rest) a.rest[r] = fabsf(rest) < INFINITY ? rest : 0.f;
       }
       o[c] = (T)(v + c < a.V ? p * g : 0.f);
     }
@@ -137,6 +145,18 @@ __device__ __forceinline__ bf16x4 read_turned(const char* p) {
   return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(shortx4*)p));
 }
 __device__ __forceinline__ bf16x8 both(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// Four columns of what rounding took from G at row m's label, times the label's row of W.
+__device__ __forceinline__ floatx4 rest_of(const float* rest, const int* labels, int m, const __bf16* W, long ldw, int c) {
+  const float x = rest[m];
+  floatx4 o{0.f, 0.f, 0.f, 0.f};
+  if (x != 0.f) {  // (then the label is one of the vocabulary)
+    const bf16x4 w = *reinterpret_cast<const bf16x4*>(W + (size_t)labels[m] * ldw + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = x * (float)w[i];
+  }
+  return o;
+}
 
 // Tile of 32 NR rows x 256 columns, 2 x WN wavefronts of 16 NR rows.  AT: A is [K][M] (m contiguous), else [M][K].  OUT: __bf16 for C itself,
 // float for the partial sums of a share of k.
@@ -170,6 +190,7 @@ __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel
   constexpr int kOut = sizeof(OUT) == 2 ? BM * kPitch * 2 : 0;
   constexpr int kRings = RA * kStageA + RB * kStageB;
   __shared__ __align__(16) char lds[kRings > kOut ? kRings : kOut];
+  __shared__ uint64_t hits[AT ? kGradRows / 64 : 1];
   char* const ringA = lds;
   char* const ringB = lds + RA * kStageA;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -325,6 +346,23 @@ __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel
   using No = std::false_type;
   if (nk > 0) {
     for (int h = AT ? -RB : -2 * RA; h < -1; ++h) load(h, h & 1);
+    if constexpr (AT) {  // which rows' labels lie in the tile, while the first halves are on their way
+      constexpr int U = 8;
+      for (int r0 = 64 * wave; r0 < a.rows; r0 += 64 * kWaves * U) {
+        int label[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int r = r0 + 64 * kWaves * u + lane;
+          label[u] = r < a.rows ? a.labels[r] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int r = r0 + 64 * kWaves * u;
+          const uint64_t is = __ballot(label[u] >= m0 && label[u] < m0 + BM);
+          if (lane == 0 && r < a.rows) hits[r / 64] = is;
+        }
+      }
+    }
     half(-1, Yes{}, No{}, Yes{});
     for (int p = 0; p < nk - 1; ++p) {
       half(2 * p, No{}, Yes{}, Yes{});
@@ -334,6 +372,35 @@ __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel
     half(nh - 1, Yes{}, Yes{}, No{});
   }
   // acc[n][t]: columns 16 t + 4 g .. + 3 of row 16 n + i16 of the wavefront's tile
+  if constexpr (AT) {
+    // What rounding took from G at a row's label, which outweighs the row's other elements together (its error would be that of the whole row): a
+    // multiply with one k for each of the tile's labels.
+    for (int q0 = 0; q0 < a.rows; q0 += 64 * 64) {
+      const uint64_t here = q0 + 64 * lane < a.rows ? hits[q0 / 64 + lane] : 0;
+      for (uint64_t some = __ballot(here != 0); some; some &= some - 1) {
+        const int q = __builtin_ctzll(some);
+        uint64_t mine = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(here >> 32), q) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)here, q);
+        for (; mine; mine &= mine - 1) {
+          const int r = q0 + 64 * q + __builtin_ctzll(mine), row = a.labels[r] - (m0 + wm * NR * 16);
+          const __bf16 rest = (__bf16)a.rest[r];
+          bf16x8 x[kColumns];
+#pragma unroll
+          for (int t = 0; t < kColumns; ++t) {
+            x[t] = bf16x8{};
+            x[t][0] = a.B[(size_t)r * a.ldb + min(n0 + (wn * kColumns + t) * 16 + i16, a.N - 1)];
+            if (g != 0) x[t][0] = (__bf16)0.f;
+          }
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            bf16x8 y{};
+            if (g == 0 && row == n * 16 + i16) y[0] = rest;
+#pragma unroll
+            for (int t = 0; t < kColumns; ++t) acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[t], y, acc[n][t], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
   if constexpr (sizeof(OUT) == 4) {
     float* C = (float*)a.C + (size_t)share * a.stride;
 #pragma unroll
@@ -355,9 +422,14 @@ __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel
     for (int n = 0; n < NR; ++n)
 #pragma unroll
       for (int t = 0; t < kColumns; ++t) {
+        floatx4 x = acc[n][t];
+        if constexpr (!AT) {
+          const int m = m0 + (wm * NR + n) * 16 + i16, c = n0 + (wn * kColumns + t) * 16 + 4 * g;
+          if (m < a.M && c < a.N) x += rest_of(a.rest, a.labels, m, a.B, a.ldb, c);
+        }
         bf16x4 o;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o[c] = (__bf16)acc[n][t][c];
+        for (int c = 0; c < 4; ++c) o[c] = (__bf16)x[c];
         *reinterpret_cast<bf16x4*>(tile + ((wm * NR + n) * 16 + i16) * kPitch + (wn * kColumns + t) * 16 + 4 * g) = o;
       }
     lds_barrier();
@@ -372,7 +444,8 @@ __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel
 
 // Sum of the shares' partial sums, in their order.
 template <class OUT>
-__global__ __launch_bounds__(256) void grad_sum_kernel(const float* part, int shares, size_t stride, size_t n, OUT* out) {
+__global__ __launch_bounds__(256) void grad_sum_kernel(const float* part, int shares, size_t stride, size_t n, OUT* out, const float* rest, const int* labels,
+                                                       const __bf16* W, int d) {
   const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (i >= n) return;
   floatx4 s = *reinterpret_cast<const floatx4*>(part + i);
@@ -384,6 +457,7 @@ __global__ __launch_bounds__(256) void grad_sum_kernel(const float* part, int sh
     for (int j = 0; j < 8; ++j)
       if (j0 + j < shares) s += x[j];
   }
+  if (rest) s += rest_of(rest, labels, (int)(i / d), W, d, (int)(i % d));  // (bf16: d is a multiple of 64)
 #pragma unroll
   for (int c = 0; c < 4; ++c)
     if (i + c < n) out[i + c] = (OUT)s[c];
@@ -409,10 +483,14 @@ hipError_t launch_grad_rows(const GradArgs& a, bool bf16, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t n, void* out, bool bf16, hipStream_t stream) {
+hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t n, void* out, bool bf16, const ProductArgs* of, hipStream_t stream) {
   const dim3 grid((unsigned)((n + 1023) / 1024)), threads(256);
-  if (bf16) hipLaunchKernelGGL(grad_sum_kernel<__bf16>, grid, threads, 0, stream, part, shares, stride, n, (__bf16*)out);
-  else hipLaunchKernelGGL(grad_sum_kernel<float>, grid, threads, 0, stream, part, shares, stride, n, (float*)out);
+  const float* const rest = of ? of->rest : nullptr;
+  const int* const labels = of ? of->labels : nullptr;
+  const __bf16* const W = of ? of->B : nullptr;
+  const int d = of ? of->N : 1;
+  if (bf16) hipLaunchKernelGGL(grad_sum_kernel<__bf16>, grid, threads, 0, stream, part, shares, stride, n, (__bf16*)out, rest, labels, W, d);
+  else hipLaunchKernelGGL(grad_sum_kernel<float>, grid, threads, 0, stream, part, shares, stride, n, (float*)out, rest, labels, W, d);
   return hipGetLastError();
 }
 

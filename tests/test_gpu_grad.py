@@ -103,7 +103,7 @@ def test_more_rows_than_a_block():
 
 
 # ---- to the last bit -----------------------------------------------------------------------------
-# With h = 0 (or W = 0) every p is 1 / V; with V a power of two G is w / V, or w (1 / V - 1) rounded to bf16, and whole numbers up to 4 in
+# With h = 0 (or W = 0) every p is 1 / V; with V a power of two G is w / V, or w (1 / V - 1), whose rounding to bf16 is made good, and whole numbers up to 4 in
 # W (or h) make every product and every sum a whole number of w / V (or of the label's element) that float32 holds.
 def _rounded(x):
     return x.to(torch.bfloat16).double()
@@ -117,7 +117,7 @@ def _uniform(R, V, seed):
     on = labels >= 0
     G = _rounded((w / V)[:, None].expand(R, V).clone())
     rows = torch.nonzero(on)[:, 0]
-    G[rows, labels[rows].long()] = _rounded(w * (1.0 / V - 1.0))[rows]
+    G[rows, labels[rows].long()] = (w.double() * (1.0 / V - 1.0))[rows]
     return labels, w, G * on[:, None]
 
 
