@@ -416,14 +416,24 @@ fef_status fef_draw_logits(const fef_draw_params* prm, const void* logits, float
  * in float32, each operation rounded once, in this order (the constants are computed in 64 bits and rounded: 1 - beta1, 1 - beta2,
  * lr / (1 - beta1^t) as the rounded lr times the rounded 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)); a bf16 parameter is p rounded to nearest.
  * Without `master`, steps of a bf16 parameter below half its last bit are lost.
- * States in 8 bits (FEF_STATE_E4M3) hold m and sqrt(v): codes in OCP e4m3, 256 consecutive elements under one float32 scale, the largest
- * magnitude of the 256 / 448, each rounded to nearest.  A positive sqrt(v) that would round to 0 takes the smallest code.  A block whose
- * largest magnitude is below 2^-100 is held as zeros.  Codes and scales that start at zero are the states of step 1.  A code moves only
- * when an element changes by half a code step, 3 to 6 %, against the largest of its block; the scale follows exactly.
+ * States in 8 bits (FEF_STATE_E4M3) hold m and sqrt(v): codes in OCP e4m3, 256 consecutive elements x under one float32 scale.  With top their
+ * largest magnitude, and every fl() a rounding to float32 (e4m3() to the nearest code, ties to the even one),
+ *   code = e4m3(fl(x * fl(448 / top))),   scale = fl(top / 448),   what is held = fl(code * scale)
+ * FEF_STATE_E4M3_RECIPROCAL takes the quotients as products with rounded reciprocals, as elementwise operations on tensors take 448.0 / top and
+ * top / 448.0 on a GPU:
+ *   code = e4m3(fl(x * fl(fl(1 / top) * 448))),   scale = fl(top * fl(1 / 448))
+ * Both are as near to m and sqrt(v).  But where x lies next to the middle of two codes, one bit in the quotient gives another code, and where that
+ * element is the next step's largest, a scale that is off by up to a code step: states that one of them has left do not go on in the bits of the
+ * other (518 M elements: some 170 codes in the first step).  States of a program that holds them by elementwise operations go on in
+ * its bits with FEF_STATE_E4M3_RECIPROCAL.
+ * A positive sqrt(v) that would round to 0 takes the smallest code.  A block whose largest magnitude is below 2^-100 is held as
+ * zeros.  Codes and scales that start at zero are the states of step 1.  A code moves only when an element changes by half a code step, 3 to
+ * 6 %, against the largest of its block; the scale follows exactly.
  * A gradient that is no finite number makes its element's p, m and v NaN or infinite, in 8 bits its whole block of states. */
 typedef enum {
   FEF_STATE_F32 = 0, /* m and v float32 [n]                                                          */
-  FEF_STATE_E4M3 = 1 /* m and v bytes [n], m_scale and v_scale float32 [ceil(n / 256)]                */
+  FEF_STATE_E4M3 = 1, /* m and v bytes [n], m_scale and v_scale float32 [ceil(n / 256)]               */
+  FEF_STATE_E4M3_RECIPROCAL = 3 /* the same, quotients as products with reciprocals                   */
 } fef_state_dtype;
 
 typedef struct {

@@ -21,7 +21,7 @@ FEF_GEMM_AUTO, FEF_GEMM_SKINNY, FEF_GEMM_TILED, FEF_GEMM_F32, FEF_GEMM_TILED256,
 FEF_GEMM_ROWSTREAM = 6
 FEF_MAX_K, FEF_MAX_BLOCK = 64, 4096
 FEF_PHASE_FUSED, FEF_PHASE_DRAFT, FEF_PHASE_TARGET = 0, 1, 2
-FEF_STATE_F32, FEF_STATE_E4M3 = 0, 1
+FEF_STATE_F32, FEF_STATE_E4M3, FEF_STATE_E4M3_RECIPROCAL = 0, 1, 3
 
 ABI_VERSION = 12   # FEF_ABI_VERSION of include/fef.h this binding's fef_params mirrors
 
@@ -694,10 +694,11 @@ class VerifyLogits:
 
 class AdamW:
     """One AdamW step at a time over a list of parameters (fef_adamw_step), all bf16 or all float32, contiguous.  `grads`: their
-    gradients, all of one of these types.  states "f32" or "8bit" (e4m3 codes and a scale per 256 elements).  `master`: True for float32
-    copies of bf16 parameters, made here, or a list of them.  `weight_decay`: one for all or one for each.  m, v (and m_scale, v_scale)
-    go on from given states; left out, they start at zero.  `schedule` (device float32 [3]: lr, 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t))
-    replaces lr and the step count, `grad_scale` (device float32 [1]) multiplies the gradients.
+    gradients, all of one of these types.  states "f32", "8bit" (e4m3 codes and a scale per 256 elements), or "8bit-reciprocal": the same in
+    the bits of elementwise torch on the GPU, whose quotients of codes and scales are products with reciprocals.  `master`: True for
+    float32 copies of bf16 parameters, made here, or a list of them.  `weight_decay`: one for all or one for each.  m, v (and m_scale,
+    v_scale) go on from given states; left out, they start at zero.  `schedule` (device float32 [3]: lr, 1 / (1 - beta1^t),
+    1 / sqrt(1 - beta2^t)) replaces lr and the step count, `grad_scale` (device float32 [1]) multiplies the gradients.
     Holds the tensors; their contents may change between steps (a backward pass writes the gradients), the tensors themselves may
     not be exchanged.  `lr` and `step_count` may be set between steps; a step adds one to `step_count` first."""
 
@@ -706,9 +707,9 @@ class AdamW:
         self.params, self.grads, self.lr, self.step_count = list(params), list(grads), lr, step
         n = len(self.params)
         assert n and len(self.grads) == n, "a gradient per parameter"
-        assert states in ("f32", "8bit")
+        assert states in ("f32", "8bit", "8bit-reciprocal")
         self.device = self.params[0].device
-        eight = states == "8bit"
+        eight = states != "f32"
 
         def made(given, default):
             out = [default(p) for p in self.params] if given is None or given is True or len(given) == 0 else list(given)
@@ -751,7 +752,7 @@ class AdamW:
         self.schedule, self.grad_scale = schedule, grad_scale
         self._params = fef_adamw_params(ctypes.sizeof(fef_adamw_params), FEF_BF16 if self.params[0].dtype == torch.bfloat16 else FEF_F32,
                                         FEF_BF16 if self.grads[0].dtype == torch.bfloat16 else FEF_F32,
-                                        FEF_STATE_E4M3 if eight else FEF_STATE_F32, lr, betas[0], betas[1], eps, max(step, 1), _ptr(schedule),
+                                        {"f32": FEF_STATE_F32, "8bit": FEF_STATE_E4M3}.get(states, FEF_STATE_E4M3_RECIPROCAL), lr, betas[0], betas[1], eps, max(step, 1), _ptr(schedule),
                                         _ptr(grad_scale), None)
 
     def step(self):

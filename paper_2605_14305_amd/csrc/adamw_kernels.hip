@@ -72,9 +72,18 @@ __device__ __forceinline__ void decode4(float (&x)[4], const uint8_t (&code)[4],
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
   x[0] = lo[0] * scale; x[1] = lo[1] * scale; x[2] = hi[0] * scale; x[3] = hi[1] * scale;
 }
+// The two quotients of a block's codes and scale, in one rounding each or by reciprocals, as the header says: one bit here moves the elements next
+// to the middle of two codes.
+__device__ __forceinline__ float of_448(float top, int reciprocal) {
+  const float q = (reciprocal ? 1.f : 448.f) / top;  // one division, whichever it is
+  return reciprocal ? q * 448.f : q;
+}
+__device__ __forceinline__ float scale_of(float top, int reciprocal) {
+  return reciprocal ? top * (1.f / 448.f) : top / 448.f;
+}
 // (top is 0 where the block is held as zeros)
-__device__ __forceinline__ void encode4(uint8_t (&code)[4], const float (&x)[4], float top) {
-  const float inv = 448.f / top;
+__device__ __forceinline__ void encode4(uint8_t (&code)[4], const float (&x)[4], float top, int reciprocal) {
+  const float inv = of_448(top, reciprocal);
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
   w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, w, true);
   w = top == 0.f ? 0 : w;
@@ -139,15 +148,15 @@ __device__ __forceinline__ void adamw_chunk(const AdamwConst& c, const AdamwTens
           if (at[u] + j >= t.n) mf[j] = r[j] = 0.f;
       }
       const float mt = top_of(mf), vt = top_of(r);
-      encode4(m[u], mf, mt);
-      encode4(v[u], r, vt);
+      encode4(m[u], mf, mt, c.reciprocal);
+      encode4(v[u], r, vt, c.reciprocal);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (vt > 0.f && r[j] > 0.f && v[u][j] == 0) v[u][j] = 1;  // the smallest code: a step is never divided by eps alone for lack of bits
       if (lane == 0 && at[u] < t.n) {
         const long unit = at[u] / kBlock;
-        t.m_scale[unit] = mt / 448.f;
-        t.v_scale[unit] = vt / 448.f;
+        t.m_scale[unit] = scale_of(mt, c.reciprocal);
+        t.v_scale[unit] = scale_of(vt, c.reciprocal);
       }
     } else {
 #pragma unroll

@@ -918,7 +918,7 @@ fef_status check_adamw(const fef_adamw_params* p, const fef_adamw_tensor* ts, in
   if (count > 0 && !ts) return fail(FEF_ERR_INVALID_ARG, "tensors is NULL with count %d", count);
   if (p->dtype != FEF_BF16 && p->dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
   if (p->grad_dtype != FEF_BF16 && p->grad_dtype != FEF_F32) return fail(FEF_ERR_INVALID_ARG, "unknown grad_dtype %d", p->grad_dtype);
-  if (p->state_dtype != FEF_STATE_F32 && p->state_dtype != FEF_STATE_E4M3)
+  if (p->state_dtype != FEF_STATE_F32 && p->state_dtype != FEF_STATE_E4M3 && p->state_dtype != FEF_STATE_E4M3_RECIPROCAL)
     return fail(FEF_ERR_INVALID_ARG, "unknown state_dtype %d", p->state_dtype);
   if (!(std::fabs(p->lr) <= 1e30)) return fail(FEF_ERR_INVALID_ARG, "lr must be a finite number");
   if (!(p->beta1 >= 0 && (float)p->beta1 < 1.f) || !(p->beta2 >= 0 && (float)p->beta2 < 1.f))
@@ -928,7 +928,7 @@ fef_status check_adamw(const fef_adamw_params* p, const fef_adamw_tensor* ts, in
   if (((uintptr_t)p->schedule | (uintptr_t)p->grad_scale) & 3)
     return fail(FEF_ERR_INVALID_ARG, "schedule and grad_scale must be 4-byte aligned");
   if (count == 0) return FEF_OK;
-  const bool eight = p->state_dtype == FEF_STATE_E4M3;
+  const bool eight = p->state_dtype != FEF_STATE_F32;
   const uintptr_t pa = p->dtype == FEF_BF16 ? 1 : 3, ga = p->grad_dtype == FEF_BF16 ? 1 : 3, sa = eight ? 0 : 3;
   std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[(size_t)count * 7 + 2]);
   if (!ranges) return fail(FEF_ERR_UNSUPPORTED, "no host memory for the check of %d tensors", count);
@@ -984,7 +984,8 @@ fef_status fef_adamw_step(const fef_adamw_params* prm, const fef_adamw_tensor* t
   c.c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(prm->beta2, (double)prm->step)));
   c.eps = (float)prm->eps;
   c.schedule = prm->schedule; c.grad_scale = prm->grad_scale;
-  const bool eight = prm->state_dtype == FEF_STATE_E4M3;
+  const bool eight = prm->state_dtype != FEF_STATE_F32;
+  c.reciprocal = prm->state_dtype == FEF_STATE_E4M3_RECIPROCAL;
   fef::AdamwTensor some[fef::kAdamwTensors];  // a launch's worth at a time
   for (int32_t i = 0; i < count;) {
     int k = 0;

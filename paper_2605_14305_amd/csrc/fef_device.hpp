@@ -207,6 +207,7 @@ struct AdamwConst {
   float lr, c1, c2, b1, one_b1, b2, one_b2, eps;  // c1 = 1 / (1 - b1^t), c2 = 1 / sqrt(1 - b2^t)
   const float* schedule;    // [3] lr, c1, c2 on the device, or NULL
   const float* grad_scale;  // or NULL
+  int reciprocal;           // states in 8 bits: quotients as products with reciprocals
 };
 struct AdamwTensor {
   void* param;
