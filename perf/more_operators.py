@@ -175,7 +175,8 @@ def prepare(case, seed):
                 s[key + "_scale"].append(scale)
     if own:
         from paper_2605_14305_amd import binding as fb
-        s["call"] = fb.AdamW(s["params"], s["grads"], lr=_LR, betas=(_B1, _B2), eps=_EPS, weight_decay=_WD, states=c["state"], master=s["master"],
+        s["call"] = fb.AdamW(s["params"], s["grads"], lr=_LR, betas=(_B1, _B2), eps=_EPS, weight_decay=_WD, master=s["master"],
+                             states={"8bit": "8bit-reciprocal"}.get(c["state"], c["state"]),  # the states above are elementwise torch's
                              m=s["m"], v=s["v"], m_scale=s["m_scale"], v_scale=s["v_scale"], step=s["t"])
     return s
 
