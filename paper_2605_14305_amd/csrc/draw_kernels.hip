@@ -273,6 +273,14 @@ struct Fixed {
   }
 };
 
+// In front of stores to places of the row that other wavefronts have written already: behind it their stores have landed.  (A barrier alone does
+// not wait for stores, __syncthreads() neither.)  The comment in the assembly is what a check of the order goes by.
+__device__ __forceinline__ void written_again() {
+  wait_newer<0>();
+  lds_barrier();
+  asm volatile("; places of the row are written again" ::: "memory");
+}
+
 struct Limits {
   unsigned k;      // 0: none
   double p;        // >= 1: none
@@ -771,7 +779,7 @@ __device__ __forceinline__ void resolve(Shared& s, const Row<BF16>& r, const Lim
   } else {
     last = (unsigned)(s.list[0] >> 32) + 1;  // (a zone has tokens)
   }
-  __syncthreads();  // waits for the stores of step 3 too, some of which these overwrite
+  written_again();  // -inf of step 3
   for (unsigned i = tid; i < kept; i += T) {
     const float y = y_of(i);
     const int id = (int)~(unsigned)s.list[i];
@@ -864,6 +872,7 @@ __device__ __forceinline__ void resolve_by_reading(Shared& s, const Row<BF16>& r
     lds_barrier();
   }
   last_id = (int)s.found[2];
+  written_again();
   // what the zone keeps
   const int lowest = by_p(lim) ? z.p_low : z.bin_k;
   unsigned kept = 0;
@@ -1055,6 +1064,7 @@ __host__ __device__ inline int tile_log_of(int V) {  // tiles of 2^this position
 // A row that is left: all bins, the middle one 31 below the maximum, and step 4 by readings.
 template <int T, bool BF16>
 __device__ __forceinline__ void left_row(const DrawArgs& a, int row, Shared& s) {
+  written_again();  // what was kept before the row was left
   Row<BF16> r;
   Limits lim;
   set_up(a, row, r, lim);
@@ -1062,7 +1072,6 @@ __device__ __forceinline__ void left_row(const DrawArgs& a, int row, Shared& s) 
   set_powers(s);
   const Fixed fixed(a.V);
   const int tile_log = tile_log_of(a.V);
-  lds_barrier();
   clear<T>(s);
   lds_barrier();
   float high = -INFINITY;
