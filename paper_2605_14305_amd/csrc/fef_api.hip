@@ -716,7 +716,7 @@ fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, con
         p.M = rows; p.N = prm->d; p.K = (int)L.ldl; p.shares = std::min(fef::grad_h_shares(rows, prm->d, prm->V), L.shares_h); p.stride = stride_h;
         p.C = p.shares > 1 ? (void*)part : (void*)gh;
         err = fef::launch_grad_h(p, stream);
-        if (err == hipSuccess && p.shares > 1) err = fef::launch_grad_sum(part, p.shares, stride_h, n_h, gh, true, &p, stream);
+        if (err == hipSuccess && p.shares > 1) err = fef::launch_grad_sum(part, p.shares, stride_h, n_h, gh, true, g.labels, p.N, g.rest, p.B, stream);
       }
       if (err == hipSuccess && grad_w) {
         fef::ProductArgs p{};
@@ -725,16 +725,16 @@ fef_status fef_head_cross_entropy_grad(const fef_params* prm, const void* h, con
         p.M = prm->V; p.N = prm->d; p.K = g.padded; p.shares = 1; p.n_first = 1;
         p.C = L.blocks > 1 ? (void*)acc : grad_w; p.add = b > 0;
         err = fef::launch_grad_w(p, L.blocks > 1, stream);
-        if (err == hipSuccess && L.blocks > 1 && b + 1 == L.blocks) err = fef::launch_grad_sum(acc, 1, 0, n_w, grad_w, true, nullptr, stream);
+        if (err == hipSuccess && L.blocks > 1 && b + 1 == L.blocks) err = fef::launch_grad_sum(acc, 1, 0, n_w, grad_w, true, nullptr, 1, nullptr, nullptr, stream);
       }
     } else {
       if (grad_h) {
         fef::ProductF32Args p{};
         p.A = (const float*)g.G; p.lda = L.ldl; p.B = (const float*)W_vocab; p.b_rows = prm->V; p.M = rows; p.N = prm->d; p.K = (int)L.ldl;
         p.shares = std::min(fef::grad_f32_shares(rows, prm->d, prm->V), L.shares_h); p.stride = stride_h;
-        p.C = p.shares > 1 ? part : (float*)gh;
+        p.C = p.shares > 1 ? part : (float*)gh; p.labels = p.shares > 1 ? nullptr : g.labels;
         err = fef::launch_grad_product_f32(p, false, stream);
-        if (err == hipSuccess && p.shares > 1) err = fef::launch_grad_sum(part, p.shares, stride_h, n_h, gh, false, nullptr, stream);
+        if (err == hipSuccess && p.shares > 1) err = fef::launch_grad_sum(part, p.shares, stride_h, n_h, gh, false, g.labels, p.N, nullptr, nullptr, stream);
       }
       if (err == hipSuccess && grad_w) {
         fef::ProductF32Args p{};

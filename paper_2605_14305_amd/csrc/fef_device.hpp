@@ -284,12 +284,14 @@ struct ProductF32Args {
   int shares;
   size_t stride;
   int add;
+  const int* labels;  // of C's rows, which are 0 where it is negative; or NULL
 };
 hipError_t launch_grad_rows(const GradArgs& a, bool bf16, hipStream_t stream);
 int grad_h_shares(int rows, int d, int V);
 hipError_t launch_grad_h(const ProductArgs& a, hipStream_t stream);
 hipError_t launch_grad_w(const ProductArgs& a, bool partial, hipStream_t stream);
-hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t n, void* out, bool bf16, const ProductArgs* of, hipStream_t stream);
+hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t n, void* out, bool bf16, const int* labels, int d, const float* rest,
+                           const __bf16* W, hipStream_t stream);
 int grad_f32_shares(int M, int N, int K);
 hipError_t launch_grad_product_f32(const ProductF32Args& a, bool at, hipStream_t stream);
 

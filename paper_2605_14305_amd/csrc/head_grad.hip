@@ -146,16 +146,18 @@ __device__ __forceinline__ bf16x4 read_turned(const char* p) {
 }
 __device__ __forceinline__ bf16x8 both(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// Four columns of what rounding took from G at row m's label, times the label's row of W.
-__device__ __forceinline__ floatx4 rest_of(const float* rest, const int* labels, int m, const __bf16* W, long ldw, int c) {
+// Four columns of row m of grad_h, to which its sum is added what rounding took from G at the label, times the label's row of W.  A row that
+// does not count is 0, also where W holds a NaN or an infinity, which its zeros of G have been multiplied by.
+__device__ __forceinline__ floatx4 with_rest(floatx4 sum, const float* rest, const int* labels, int m, const __bf16* W, long ldw, int c) {
+  const int label = labels[m];
+  if (label < 0) return floatx4{0.f, 0.f, 0.f, 0.f};
   const float x = rest[m];
-  floatx4 o{0.f, 0.f, 0.f, 0.f};
   if (x != 0.f) {  // (then the label is one of the vocabulary)
-    const bf16x4 w = *reinterpret_cast<const bf16x4*>(W + (size_t)labels[m] * ldw + c);
+    const bf16x4 w = *reinterpret_cast<const bf16x4*>(W + (size_t)label * ldw + c);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = x * (float)w[i];
+    for (int i = 0; i < 4; ++i) sum[i] += x * (float)w[i];
   }
-  return o;
+  return sum;
 }
 
 // Tile of 32 NR rows x 256 columns, 2 x WN wavefronts of 16 NR rows.  AT: A is [K][M] (m contiguous), else [M][K].  OUT: __bf16 for C itself,
@@ -425,7 +427,7 @@ __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel
         floatx4 x = acc[n][t];
         if constexpr (!AT) {
           const int m = m0 + (wm * NR + n) * 16 + i16, c = n0 + (wn * kColumns + t) * 16 + 4 * g;
-          if (m < a.M && c < a.N) x += rest_of(a.rest, a.labels, m, a.B, a.ldb, c);
+          if (m < a.M && c < a.N) x = with_rest(x, a.rest, a.labels, m, a.B, a.ldb, c);
         }
         bf16x4 o;
 #pragma unroll
@@ -442,10 +444,10 @@ __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel
   }
 }
 
-// Sum of the shares' partial sums, in their order.
+// Sum of the shares' partial sums, in their order.  With labels: of grad_h, whose rows that do not count are 0; rest: and bf16.
 template <class OUT>
-__global__ __launch_bounds__(256) void grad_sum_kernel(const float* part, int shares, size_t stride, size_t n, OUT* out, const float* rest, const int* labels,
-                                                       const __bf16* W, int d) {
+__global__ __launch_bounds__(256) void grad_sum_kernel(const float* part, int shares, size_t stride, size_t n, OUT* out, const int* labels, int d, const float* rest,
+                                                       const __bf16* W) {
   const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (i >= n) return;
   floatx4 s = *reinterpret_cast<const floatx4*>(part + i);
@@ -457,7 +459,13 @@ __global__ __launch_bounds__(256) void grad_sum_kernel(const float* part, int sh
     for (int j = 0; j < 8; ++j)
       if (j0 + j < shares) s += x[j];
   }
-  if (rest) s += rest_of(rest, labels, (int)(i / d), W, d, (int)(i % d));  // (bf16: d is a multiple of 64)
+  if (rest) {
+    s = with_rest(s, rest, labels, (int)(i / d), W, d, (int)(i % d));  // (bf16: d is a multiple of 64)
+  } else if (labels) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (i + c < n && labels[(i + c) / d] < 0) s[c] = 0.f;
+  }
 #pragma unroll
   for (int c = 0; c < 4; ++c)
     if (i + c < n) out[i + c] = (OUT)s[c];
@@ -483,14 +491,11 @@ hipError_t launch_grad_rows(const GradArgs& a, bool bf16, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t n, void* out, bool bf16, const ProductArgs* of, hipStream_t stream) {
+hipError_t launch_grad_sum(const float* part, int shares, size_t stride, size_t n, void* out, bool bf16, const int* labels, int d, const float* rest,
+                           const __bf16* W, hipStream_t stream) {
   const dim3 grid((unsigned)((n + 1023) / 1024)), threads(256);
-  const float* const rest = of ? of->rest : nullptr;
-  const int* const labels = of ? of->labels : nullptr;
-  const __bf16* const W = of ? of->B : nullptr;
-  const int d = of ? of->N : 1;
-  if (bf16) hipLaunchKernelGGL(grad_sum_kernel<__bf16>, grid, threads, 0, stream, part, shares, stride, n, (__bf16*)out, rest, labels, W, d);
-  else hipLaunchKernelGGL(grad_sum_kernel<float>, grid, threads, 0, stream, part, shares, stride, n, (float*)out, rest, labels, W, d);
+  if (bf16) hipLaunchKernelGGL(grad_sum_kernel<__bf16>, grid, threads, 0, stream, part, shares, stride, n, (__bf16*)out, labels, d, rest, W);
+  else hipLaunchKernelGGL(grad_sum_kernel<float>, grid, threads, 0, stream, part, shares, stride, n, (float*)out, labels, d, rest, W);
   return hipGetLastError();
 }
 

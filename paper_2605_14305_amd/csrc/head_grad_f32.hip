@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void grad_product_f32_kernel(ProductF32Ar
         for (int i = 0; i < 4; ++i)
           if (c + i < a.N) {
             float* p = C + (size_t)m * a.N + c + i;
-            *p = a.add ? *p + acc[n][t][i] : acc[n][t][i];
+            *p = a.labels && a.labels[m] < 0 ? 0.f : a.add ? *p + acc[n][t][i] : acc[n][t][i];
           }
     }
 }
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(kThreads, 2) void grad_product_f32_wide_kernel(Prod
       const int m = m0 + (wm * MT + n) * 16 + i16, c = n0 + (wn * NT + t) * 16 + 4 * g;
       if (m < a.M && c < a.N) {
         floatx4* p = reinterpret_cast<floatx4*>(C + (size_t)m * a.N + c);
-        *p = a.add ? *p + acc[n][t] : acc[n][t];
+        *p = a.labels && a.labels[m] < 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : a.add ? *p + acc[n][t] : acc[n][t];
       }
     }
 }
