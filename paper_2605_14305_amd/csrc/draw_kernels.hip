@@ -81,11 +81,12 @@ __device__ __forceinline__ double horner(double t, double p, double c) {
   asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(t), "v"(p), "s"(c));
   return r;
 }
-// exp(x) for x <= 1, to 2^-51 or so; each step one rounding, so that the same x gives the same bits wherever this is compiled into.
+// exp(x) for x <= 1, to 2^-51 or so; each step one rounding, so that the same x gives the same bits wherever this is compiled into.  x = (64 i + j) ln 2 / 64 + q:
+// 2^i, 2^(j / 64) from a table and a Taylor polynomial in q, the table-driven way that P. T. P. Tang published (ACM TOMS 15, 1989).
 __device__ __forceinline__ double exp64(double x, const double* power) {
   x = fmax(x, -800.0);  // 0
   const double k = rint(x * 92.332482616893657);  // 64 / ln 2
-  const double r = fma(k, -1.0830424696249145e-02, x), q = fma(k, -3.6219510595213e-19, r);  // ln 2 / 64 in two parts
+  const double r = fma(k, -1.0830424696249145e-02, x), q = fma(k, -3.623510646634843e-19, r);  // ln 2 / 64 in two parts
   const int j = (int)k;
   const double p = horner(q, horner(q, horner(q, horner(q, horner(q, 1.0 / 120, 1.0 / 24), 1.0 / 6), 1.0 / 2), 1.0), 1.0);
   return ldexp(power[j & 63] * p, j >> 6);
