@@ -427,8 +427,13 @@ fef_status fef_draw_logits(const fef_draw_params* prm, const void* logits, float
  * other (518 M elements: some 170 codes in the first step).  States of a program that holds them by elementwise operations go on in
  * its bits with FEF_STATE_E4M3_RECIPROCAL.
  * A positive sqrt(v) that would round to 0 takes the smallest code.  A block whose largest magnitude is below 2^-100 is held as
- * zeros.  Codes and scales that start at zero are the states of step 1.  A code moves only when an element changes by half a code step, 3 to
- * 6 %, against the largest of its block; the scale follows exactly.
+ * zeros.  Codes and scales that start at zero are the states of step 1.
+ * A code moves only when an element changes by half a code step, 3 to 6 %, against the largest of its block; the scale follows exactly.  So
+ * sqrt(v) falls against its block's largest only where a step takes 3 to 6 % off it, which beta2 = 0.95 is near to and 0.999 (0.05 % a step) is
+ * not, and with 0.999 it rises only where |g| is some 8 sqrt(v) or more.  After a thousand steps on gaussian gradients, each element with a spread of its
+ * own, what is held is 0.83 to 1.20 times the exact sqrt(v) with beta2 = 0.95, 0.72 to 1.55 times with 0.999 (1 % to 99 % of the elements; all of one
+ * spread 0.86 to 1.31, 0.64 to 1.58).  Where half of a block's elements turn ten times quieter, with 0.999 a thousand steps later theirs is 1.5 to 1.8
+ * times too large in the middle and 2.7 at 99 %.
  * A gradient that is no finite number makes its element's p, m and v NaN or infinite, in 8 bits its whole block of states. */
 typedef enum {
   FEF_STATE_F32 = 0, /* m and v float32 [n]                                                          */
