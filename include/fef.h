@@ -271,9 +271,10 @@ fef_status fef_head_cross_entropy(const fef_params* prm, const void* h, const vo
  *   grad_w   [V, d] device, dtype prm->dtype, 16-byte aligned; NULL: not wanted, but not both
  * The gradients are written whole, whatever was there.  A row whose label is negative has no part in any of it: its CE and its row of
  * grad_h are 0, and h is not looked at there for grad_w.  A label >= V makes the row's CE and grad_h NaN, and grad_w with them.
- * bf16: the logits are float32, G is rounded to bf16 (half a step of 2^-8 of each element) as an operand of the matrix cores, sums are held in
- * 32 bits, grad_h and grad_w are rounded once.  f32: float32 throughout.  Rows are taken 8192 at a time; the order of all sums
- * depends on the sizes alone.
+ * bf16: the logits are float32, G is rounded to bf16 (by 2^-8 of each element at the most) as an operand of the matrix cores, sums are held in 32
+ * bits, grad_h and grad_w are rounded once.  What the rounding takes from a row's element at its label, which is as large as the row's others
+ * together, is added to both sums again (to grad_h as it is, to grad_w in bf16, so that 2^-16 of the element is lost at the most).  f32: float32
+ * throughout.  Rows are taken 8192 at a time; the order of all sums depends on the sizes alone.
  * Fields of prm that are read: struct_size, d, V (at most 2^29), dtype, temperature (1 / tau finite), gemm_variant (AUTO, or what AUTO takes: TILED256 or
  * F32), workspace, workspace_bytes (at least fef_cross_entropy_grad_workspace_bytes, which depends on R, d, V and dtype alone; 0 if the
  * arguments are invalid), stream.  ev_head_begin and ev_head_end must be NULL.  bf16: d a positive multiple of 64.  1 <= R <= 2^24.

@@ -13,14 +13,17 @@
 //   4. the list is sorted; rank and mass before each of its tokens give (T, I); what it keeps is written.
 //   5. the token: sums of the kept mass per tile of ids, then the ids of one tile.
 //
-// Masses decide which token is the last, so they are exact to 2^-44 or so: a weight is computed in 64 bits and added as a whole number of
-// 2^-f, which no order of the atomics changes.  In step 1 weights are relative to their bin's middle, |y - middle| <= 1/64, where a
-// polynomial of degree 5 is exact to 2^-45.
+// Masses decide which token is the last: a weight is computed in 64 bits and added as a whole number of 2^-s, s = min(50, 61 - the bits of V), which no
+// order of the atomics changes.  In step 1 weights are relative to their bin's middle, |y - middle| <= 1/64, where a polynomial of degree 5
+// is exact to 2^-45, so a bin's mass is off by 2^-(s + 1) of itself at the most, and by 2^-45: s = 44 up to V = 131071, 43 at 151936, 38 at 2^22, 31 at
+// 2^29.  A border nearer to a mass than that is decided by rounding.
 //
 // Two ways through these steps.  draw_rows_kernel: a workgroup per row.  Slices of a row, a workgroup each, in three launches:
 // draw_bins_kernel (step 1), draw_keep_kernel (steps 2 and 3: every workgroup adds up its row's bins) and draw_finish_kernel (a workgroup per
 // row: steps 4 and 5).  What this does not serve (a list longer than kList: equal logits; limits that end below step 2's bins; a maximum far
-// above the sample) is left to left_row, which narrows down the last key by readings of the row, 12 bits each.
+// above the sample) is left to left_row, which narrows down the last key by readings of the row, 12 bits each: slow, some 270 to 310 us for 8 rows whose
+// grammar leaves 5 tokens with negative logits (none in the sample: ref is 0), 510 to 600 where a bin's list is too long (gaussian logits of
+// deviation 0.7, p = 0.8), up to 1900 where all logits are equal (V = 126464 and 151936; 28 to 63 us where the row is not left).
 // Which way, with k = 100 and p = 0.95 / p = 0.95 alone, a workgroup per row against slices:
 //   8 rows of V = 12000 23.0 / 20.6 against 27.9 / 26.4 us, 16384 24.9 / 27.2 against 28.0 / 29.5, 24000 29.0 / 33.5 against 28.1 / 31.1: one launch
 //   below kShort tokens;

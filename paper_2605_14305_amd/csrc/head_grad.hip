@@ -176,8 +176,9 @@ __device__ __forceinline__ floatx4 with_rest(floatx4 sum, const float* rest, con
 //     multiplies.  Two workgroups per CU, in 72 KB each, work under each other's ends: 1903 us, against 1963 with
 //     one of 256 x 256; 48 rows 290 -> 273, 333 rows of d = 2048, V = 50257 128 -> 112 (with stores past the caches 263 and 102).  An XCD walks
 //     down a strip of kStrip tiles, whose columns of H (4 MB at 2048 rows) stay in its L2: 1740 us = 1.22 PFLOP/s, 4.3 GB read (strips of 8 tiles
-//     1785 us, 6.2 GB; rows of all 16 1898 us, 12.0 GB).  These figures are without the labels' rounding made good, which costs some 80 us at 48 rows and
-//     250 at 2048, and takes the gradients' error against 64 bits from 0.0024 to 0.0018 of their norm.
+//     1785 us, 6.2 GB; rows of all 16 1898 us, 12.0 GB).  With the labels' rounding made good, which takes the
+//     gradients' error against 64 bits from 0.0024 to 0.0018 of their norm, 30 registers are spilled and the kernel takes 1976 us (1.07 PFLOP/s, 4.7 GB
+//     read, 1.5 GB written, a third of it spills), 373 at 48 rows, 143 at 333.
 template <int NR, int WN, bool AT, class OUT>
 __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel(ProductArgs a) {
   constexpr int BM = 16 * NR * WM, kWaves = WM * WN, kThreads = kWave * kWaves, kColumns = BN / WN / 16;
@@ -377,8 +378,10 @@ __global__ __launch_bounds__(128 * WN, WN == 2 ? 2 : 1) void grad_product_kernel
   }
   // acc[n][t]: columns 16 t + 4 g .. + 3 of row 16 n + i16 of the wavefront's tile
   if constexpr (AT) {
-    // What rounding took from G at a row's label, which outweighs the row's other elements together (its error would be that of the whole row): a
-    // multiply with one k for each of the tile's labels.
+    // What rounding took from G at a row's label: that element is as large as all others of its row together, so its one rounding is most of the row's
+    // error, while theirs are many and independent.  (In a row that is sure of another token that token's element is as large, and its rounding
+    // stays.)  A multiply with one k for each of the tile's labels; its time hardly depends on how they lie: 2048 rows of d = 4096, V = 126464 5.53 ms
+    // with labels drawn uniformly, 5.56 by 1 / rank, 5.49 with one label for all; 8192 rows 24.8, 25.7, 25.1.
     for (int q0 = 0; q0 < a.rows; q0 += 64 * 64) {
       const uint64_t here = q0 + 64 * lane < a.rows ? hits[q0 / 64 + lane] : 0;
       for (uint64_t some = __ballot(here != 0); some; some &= some - 1) {
